@@ -1,0 +1,432 @@
+// Kernels around a paged key/value cache (include/lssvm_cache.h): rotary positions,
+// writing new tokens, eviction by weight. All of them move memory; what they compute
+// hides behind that.
+#include "cache_internal.h"
+
+#include <algorithm>
+
+namespace lssvm {
+namespace {
+
+constexpr int kThreads = 256;
+
+// ------------------------------------------------------ rotary positions ----
+
+// cos and sin of `angle`, to about an ulp of fp32: the quarter turns are taken off in
+// fp64 (pi/2 in two parts), so that positions of millions lose nothing.
+LSSVM_DEV void turn(double angle, float* c, float* s) {
+  const double k = rint(angle * 0.63661977236758134308);
+  double r = fma(-k, 1.57079632679489655800, angle);
+  r = fma(-k, 6.12323399573676603587e-17, r);
+  float sr, cr;
+  sincosf((float)r, &sr, &cr);
+  const int quarter = (int)((int64_t)k & 3);
+  const float a = quarter & 1 ? sr : cr, b = quarter & 1 ? cr : sr;
+  *c = quarter == 1 || quarter == 2 ? -a : a;
+  *s = quarter >= 2 ? -b : b;
+}
+
+// A head's values are handled in chunks of 16 bytes: first those of the turned part
+// (half layout: 16 bytes from either half), then those that are copied.
+template <typename T>
+__host__ __device__ inline int pair_chunks(int pairs, bool interleaved) {
+  const int v = interleaved ? kVec<T> / 2 : kVec<T>;
+  return (pairs + v - 1) / v;
+}
+template <typename T>
+__host__ __device__ inline int copy_chunks(int values) {
+  return (values + kVec<T> - 1) / kVec<T>;
+}
+
+// The factors of the pairs of chunk `at`.
+template <typename T, bool INTER>
+struct Factors {
+  static constexpr int N = INTER ? kVec<T> / 2 : kVec<T>;
+  float c[N], s[N];
+  LSSVM_DEV void set(const RotaryArgs& a, int64_t t, int at) {
+    const double p = a.wide_positions
+                         ? (double)static_cast<const int64_t*>(a.positions)[t]
+                         : (double)static_cast<const int32_t*>(a.positions)[t];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int pair = at * N + i;
+      if (pair >= a.pairs) break;
+      turn(p * a.freqs[pair], &c[i], &s[i]);
+      c[i] *= a.scale;
+      s[i] *= a.transpose ? -a.scale : a.scale;
+    }
+  }
+};
+
+// Turns the pairs of chunk `at` of one head. All of the chunk is read before any of
+// it is written, so y may be x.
+template <typename T, bool INTER>
+LSSVM_DEV void turn_chunk(const Factors<T, INTER>& f, const T* x, T* y, int at, int pairs) {
+  constexpr int N = Factors<T, INTER>::N, W = kVec<T>;
+  const int left = pairs - at * N;
+  if constexpr (INTER) {
+    x += at * W;
+    y += at * W;
+    Loose<T, W> v;
+    if (left >= N) {
+      v = *reinterpret_cast<const Loose<T, W>*>(x);
+    } else {
+      for (int i = 0; i < 2 * left; ++i) v.v[i] = x[i];
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float p = (float)v.v[2 * i], q = (float)v.v[2 * i + 1];
+      v.v[2 * i] = (T)(p * f.c[i] - q * f.s[i]);
+      v.v[2 * i + 1] = (T)(q * f.c[i] + p * f.s[i]);
+    }
+    if (left >= N) {
+      *reinterpret_cast<Loose<T, W>*>(y) = v;
+    } else {
+      for (int i = 0; i < 2 * left; ++i) y[i] = v.v[i];
+    }
+  } else {
+    x += at * N;
+    y += at * N;
+    Loose<T, W> a, b;
+    if (left >= N) {
+      a = *reinterpret_cast<const Loose<T, W>*>(x);
+      b = *reinterpret_cast<const Loose<T, W>*>(x + pairs);
+    } else {
+      for (int i = 0; i < left; ++i) {
+        a.v[i] = x[i];
+        b.v[i] = x[i + pairs];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float p = (float)a.v[i], q = (float)b.v[i];
+      a.v[i] = (T)(p * f.c[i] - q * f.s[i]);
+      b.v[i] = (T)(q * f.c[i] + p * f.s[i]);
+    }
+    if (left >= N) {
+      *reinterpret_cast<Loose<T, W>*>(y) = a;
+      *reinterpret_cast<Loose<T, W>*>(y + pairs) = b;
+    } else {
+      for (int i = 0; i < left; ++i) {
+        y[i] = a.v[i];
+        y[i + pairs] = b.v[i];
+      }
+    }
+  }
+}
+
+// Copies chunk `at` of `n` values.
+template <typename T>
+LSSVM_DEV void copy_chunk(const T* x, T* y, int at, int n) {
+  constexpr int W = kVec<T>;
+  x += at * W;
+  y += at * W;
+  const int left = n - at * W;
+  if (left >= W) {
+    *reinterpret_cast<Loose<T, W>*>(y) = *reinterpret_cast<const Loose<T, W>*>(x);
+  } else {
+    for (int i = 0; i < left; ++i) y[i] = x[i];
+  }
+}
+
+// Heads that a thread handles one after the other with the same factors: as many as
+// leave `enough` threads, since a chunk's sines cost more than its 16 bytes, and a
+// few tokens need the threads more.
+constexpr int64_t kEnoughThreads = 256 * 1024;
+inline int heads_per_thread(int64_t tokens, int chunks, int heads) {
+  const int64_t threads = tokens * chunks * heads;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(heads, threads / kEnoughThreads));
+}
+
+// v / by and the rest; in 32 bits where they do.
+LSSVM_DEV int64_t split(int64_t v, int by, int* rest) {
+  const int64_t q = v >> 32 ? v / by : (int64_t)((uint32_t)v / (uint32_t)by);
+  *rest = (int)(v - q * by);
+  return q;
+}
+
+template <typename T, bool INTER>
+__global__ void __launch_bounds__(kThreads) k_rotary(RotaryArgs a, int chunks, int turned,
+                                                     int groups) {
+  int at, group;
+  const int64_t t = split(split((int64_t)blockIdx.x * kThreads + threadIdx.x, chunks, &at),
+                          groups, &group);
+  if (t >= a.tokens) return;
+  const T* x = static_cast<const T*>(a.x) + t * a.xs.outer;
+  T* y = static_cast<T*>(a.out) + t * a.os.outer;
+  Factors<T, INTER> f;
+  if (at < turned) f.set(a, t, at);
+  for (int h = group; h < a.heads; h += groups) {
+    const T* xh = x + h * a.xs.head;
+    T* yh = y + h * a.os.head;
+    if (at < turned)
+      turn_chunk<T, INTER>(f, xh, yh, at, a.pairs);
+    else
+      copy_chunk(xh + 2 * a.pairs, yh + 2 * a.pairs, at - turned, a.dim - 2 * a.pairs);
+  }
+}
+
+template <typename F>
+hipError_t by_dtype(int dtype, F f) {
+  if (dtype == LSSVM_BF16) return f(bf16_t{});
+  if (dtype == LSSVM_F16) return f(f16_t{});
+  return f(float{});
+}
+
+// -------------------------------------------------------- cache append ------
+
+// One chunk of a new token's key or value per thread, for some of its heads.
+template <typename T, bool INTER>
+__global__ void __launch_bounds__(kThreads) k_append(AppendArgs a, int chunks, int turned,
+                                                     int copied, int groups) {
+  int at, group;
+  const int64_t t = split(split((int64_t)blockIdx.x * kThreads + threadIdx.x, chunks, &at),
+                          groups, &group);
+  if (t >= a.k.tokens) return;
+  // the sequence: the last whose first token is not behind t
+  int lo = 0, hi = (int)a.c.sequences;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (a.offsets[mid] <= t) lo = mid; else hi = mid;
+  }
+  const int64_t first = clip(a.offsets[lo], a.k.tokens), end = clip(a.offsets[lo + 1], a.k.tokens);
+  if (t < first || t >= end) return;
+  const int64_t j = cache_length(a.c, lo) - (end - t);
+  if (j < 0) return;
+  int slot;
+  const int page = cache_page(a.c, lo, (int)j, &slot);
+  if (page < 0) return;
+  T* k = static_cast<T*>(a.c.k) + page * a.c.k_stride[0] + slot * a.c.k_stride[2];
+  T* v = static_cast<T*>(a.c.v) + page * a.c.v_stride[0] + slot * a.c.v_stride[2];
+  const T* xk = static_cast<const T*>(a.k.x) + t * a.k.xs.outer;
+  const T* xv = static_cast<const T*>(a.v) + t * a.vs.outer;
+  Factors<T, INTER> f;
+  if (at < turned) f.set(a.k, t, at);
+  for (int h = group; h < a.k.heads; h += groups) {
+    if (at < turned) {
+      turn_chunk<T, INTER>(f, xk + h * a.k.xs.head, k + h * a.c.k_stride[1], at, a.k.pairs);
+    } else if (at < turned + copied) {
+      copy_chunk(xk + h * a.k.xs.head + 2 * a.k.pairs, k + h * a.c.k_stride[1] + 2 * a.k.pairs,
+                 at - turned, a.k.dim - 2 * a.k.pairs);
+    } else {
+      copy_chunk(xv + h * a.vs.head, v + h * a.c.v_stride[1], at - turned - copied, a.k.dim);
+    }
+    if (at == chunks - 1 && a.c.weight)
+      a.c.weight[page * a.c.weight_stride[0] + h * a.c.weight_stride[1] + slot] = 0.0f;
+  }
+}
+
+// ------------------------------------------------------------- eviction -----
+
+// Floats as integers of the same order: -0 as 0, NaN below all.
+LSSVM_DEV uint32_t weight_order(float w) {
+  if (w != w) return 0;
+  const uint32_t u = __float_as_uint(w + 0.0f);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+constexpr int kSelectThreads = 1024;
+constexpr int kSelectWaves = kSelectThreads / 64;
+constexpr int kSelectKeys = 24 * 1024;   // keys of a sequence that LDS holds: 96 KB
+
+// One head of one sequence: the border, the m-th largest weight of the keys before
+// the recent ones, by four rounds over 8 bits of the ordered integers each; then the
+// kept indices in order, every wave a run of its own.
+__global__ void __launch_bounds__(kSelectThreads) k_evict_select(EvictArgs a) {
+  extern __shared__ uint32_t held[];
+  __shared__ uint32_t bins[256];
+  __shared__ uint32_t border, above;
+  __shared__ int count_over[kSelectWaves], count_equal[kSelectWaves];
+  const int s = blockIdx.x, h = blockIdx.y;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int L = cache_length(a.from, s);
+  const int n = min(L, a.budget);
+  const int recent = min(n, a.recent), old = L - recent, m = n - recent;
+  int32_t* kept = a.kept + ((int64_t)s * a.from.heads + h) * a.budget;
+  for (int i = n + tid; i < a.budget; i += kSelectThreads) kept[i] = -1;
+  if (h == 0 && tid == 0) a.to.lengths[s] = n;
+  for (int i = tid; i < recent; i += kSelectThreads) kept[m + i] = old + i;
+  if (m == 0) return;
+
+  const bool fits = old <= kSelectKeys;
+  auto fetch = [&](int j) -> uint32_t {
+    int slot;
+    const int p = cache_page(a.from, s, j, &slot);
+    return p < 0 ? 0
+                 : weight_order(a.from.weight[p * a.from.weight_stride[0] +
+                                              h * a.from.weight_stride[1] + slot]);
+  };
+  if (fits)
+    for (int j = tid; j < old; j += kSelectThreads) held[j] = fetch(j);
+  auto key = [&](int j) -> uint32_t { return fits ? held[j] : fetch(j); };
+
+  if (tid == 0) border = 0, above = 0;
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    if (tid < 256) bins[tid] = 0;
+    __syncthreads();
+    const uint32_t known = border, mask = shift == 24 ? 0 : 0xFFFFFFFFu << (shift + 8);
+    for (int j = tid; j < old; j += kSelectThreads) {
+      const uint32_t u = key(j);
+      if ((u & mask) == known) atomicAdd(&bins[(u >> shift) & 255], 1u);
+    }
+    __syncthreads();
+    if (tid < 64) {   // from the largest value down: four bins a lane
+      uint32_t c[4], sum = 0;
+      for (int i = 0; i < 4; ++i) c[i] = bins[255 - 4 * lane - i], sum += c[i];
+      uint32_t before = sum;
+      for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t o = __shfl_up(before, d);
+        if (lane >= d) before += o;
+      }
+      before = above + before - sum;
+      for (int i = 0; i < 4; ++i) {
+        if (before < (uint32_t)m && before + c[i] >= (uint32_t)m) {
+          border = known | ((uint32_t)(255 - 4 * lane - i) << shift);
+          above = before;
+        }
+        before += c[i];
+      }
+    }
+    __syncthreads();
+  }
+  const uint32_t edge = border;
+  const int equals = m - (int)above;   // of those at the border, so many first ones
+
+  const int run = ((old + kSelectWaves - 1) / kSelectWaves + 63) & ~63;
+  const int j0 = wave * run, j1 = min(old, j0 + run);
+  int over = 0, equal = 0;
+  for (int j = j0 + lane; j < j1; j += 64) {
+    const uint32_t u = key(j);
+    over += u > edge;
+    equal += u == edge;
+  }
+  for (int d = 32; d; d >>= 1) over += __shfl_xor(over, d), equal += __shfl_xor(equal, d);
+  if (lane == 0) count_over[wave] = over, count_equal[wave] = equal;
+  __syncthreads();
+  over = equal = 0;
+  for (int w = 0; w < wave; ++w) over += count_over[w], equal += count_equal[w];
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+  for (int j = j0; j < j1; j += 64) {
+    const bool in = j + lane < j1;
+    const uint32_t u = in ? key(j + lane) : 0;
+    const bool o = in && u > edge, e = in && u == edge;
+    const uint64_t bo = __ballot(o), be = __ballot(e);
+    const int mine = equal + __popcll(be & below);
+    if (o || (e && mine < equals))
+      kept[over + __popcll(bo & below) + min(mine, equals)] = j + lane;
+    over += __popcll(bo);
+    equal += __popcll(be);
+  }
+}
+
+// Rows of keys and values, 16 bytes of each per thread and row.
+constexpr int kCopyRows = 4;   // rows in flight per thread
+__global__ void __launch_bounds__(kThreads) k_evict_copy(EvictArgs a, int lanes, int size) {
+  const int s = blockIdx.z, h = blockIdx.y;
+  const int n = min(cache_length(a.from, s), a.budget);
+  const int rows = kThreads / lanes;   // rows that a block moves at once
+  const int row = threadIdx.x / lanes, at = threadIdx.x % lanes;
+  if (row >= rows) return;
+  const int32_t* kept = a.kept + ((int64_t)s * a.from.heads + h) * a.budget;
+  const int first = blockIdx.x * rows * kCopyRows + row;
+  const char* src[2][kCopyRows];
+  char* dst[2][kCopyRows];
+  bool move[kCopyRows], hole[kCopyRows];
+#pragma unroll
+  for (int r = 0; r < kCopyRows; ++r) {
+    const int i = first + r * rows;
+    move[r] = i < n;
+    hole[r] = false;
+    if (!move[r]) continue;
+    int from_slot, to_slot;
+    const int to = cache_page(a.to, s, i, &to_slot);
+    const int from = cache_page(a.from, s, kept[i], &from_slot);
+    move[r] = to >= 0;
+    hole[r] = from < 0;
+    auto place = [&](const int64_t* st, int p, int slot) {
+      return (p * st[0] + h * st[1] + slot * st[2]) * size + 16 * at;
+    };
+    src[0][r] = static_cast<const char*>(a.from.k) + place(a.from.k_stride, from, from_slot);
+    src[1][r] = static_cast<const char*>(a.from.v) + place(a.from.v_stride, from, from_slot);
+    dst[0][r] = static_cast<char*>(a.to.k) + place(a.to.k_stride, to, to_slot);
+    dst[1][r] = static_cast<char*>(a.to.v) + place(a.to.v_stride, to, to_slot);
+    if (at == 0 && move[r])
+      a.to.weight[to * a.to.weight_stride[0] + h * a.to.weight_stride[1] + to_slot] =
+          hole[r] ? 0.0f
+                  : a.from.weight[from * a.from.weight_stride[0] + h * a.from.weight_stride[1] +
+                                  from_slot];
+  }
+  uint4 w[2][kCopyRows];
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int r = 0; r < kCopyRows; ++r)
+      w[x][r] = move[r] && !hole[r] ? *reinterpret_cast<const uint4*>(src[x][r]) : uint4{};
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int r = 0; r < kCopyRows; ++r)
+      if (move[r]) *reinterpret_cast<uint4*>(dst[x][r]) = w[x][r];
+}
+
+}  // namespace
+
+hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream) {
+  return by_dtype(a.dtype, [&](auto type) {
+    using T = decltype(type);
+    const int turned = pair_chunks<T>(a.pairs, a.interleaved);
+    const bool in_place = a.x == a.out;
+    const int chunks = turned + (in_place ? 0 : copy_chunks<T>(a.dim - 2 * a.pairs));
+    if (chunks == 0) return hipSuccess;
+    const int each = heads_per_thread(a.tokens, chunks, a.heads);
+    const int groups = (a.heads + each - 1) / each;
+    const int64_t items = a.tokens * groups * chunks;
+    const dim3 grid((unsigned)((items + kThreads - 1) / kThreads));
+    if (a.interleaved)
+      k_rotary<T, true><<<grid, kThreads, 0, stream>>>(a, chunks, turned, groups);
+    else
+      k_rotary<T, false><<<grid, kThreads, 0, stream>>>(a, chunks, turned, groups);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_append(const AppendArgs& a, hipStream_t stream) {
+  return by_dtype(a.c.dtype, [&](auto type) {
+    using T = decltype(type);
+    const int turned = pair_chunks<T>(a.k.pairs, a.k.interleaved);
+    const int copied = copy_chunks<T>(a.k.dim - 2 * a.k.pairs);
+    const int chunks = turned + copied + copy_chunks<T>(a.k.dim);
+    const int each = heads_per_thread(a.k.tokens, chunks, a.k.heads);
+    const int groups = (a.k.heads + each - 1) / each;
+    const int64_t items = a.k.tokens * groups * chunks;
+    const dim3 grid((unsigned)((items + kThreads - 1) / kThreads));
+    if (a.k.interleaved)
+      k_append<T, true><<<grid, kThreads, 0, stream>>>(a, chunks, turned, copied, groups);
+    else
+      k_append<T, false><<<grid, kThreads, 0, stream>>>(a, chunks, turned, copied, groups);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_evict(const EvictArgs& a, hipStream_t stream) {
+  const int64_t most = a.from.columns * a.from.page;
+  const size_t lds = 4 * (size_t)std::min<int64_t>(most, kSelectKeys);
+  hipError_t e = hipSuccess;
+  if (lds > 32 * 1024 &&
+      (e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_evict_select),
+                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) !=
+          hipSuccess)
+    return e;
+  k_evict_select<<<dim3((unsigned)a.from.sequences, (unsigned)a.from.heads), kSelectThreads, lds,
+                   stream>>>(a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  const int size = a.from.dtype == LSSVM_F32 ? 4 : 2;
+  const int lanes = (int)a.from.dim * size / 16, rows = kThreads / lanes * kCopyRows;
+  const int64_t n = std::min<int64_t>(a.budget, most);
+  k_evict_copy<<<dim3((unsigned)((n + rows - 1) / rows), (unsigned)a.from.heads,
+                             (unsigned)a.from.sequences),
+                        kThreads, 0, stream>>>(a, lanes, size);
+  return hipGetLastError();
+}
+
+}  // namespace lssvm
