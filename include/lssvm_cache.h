@@ -41,7 +41,7 @@ enum { LSSVM_BF16 = 2, LSSVM_F16 = 3 };
  * dim contiguous values, with strides in elements; v and weight alike (a weight is
  * one float per key, its slots contiguous). Strides are free as long as no two rows
  * overlap and rows of k and v begin on 16 bytes, so heads may stand before or behind
- * the slots of a page. */
+ * the slots of a page; slots are at most 2^26 values apart. */
 typedef struct lssvm_cache {
     void* k;
     void* v;
@@ -53,7 +53,7 @@ typedef struct lssvm_cache {
     int64_t page;            /* keys per page, >= 1                               */
     int64_t dim;             /* values per key and head, a multiple of 8, 8 .. 256 */
     int64_t sequences;       /* 1 .. 65535                                        */
-    int64_t columns;         /* columns of table, >= 1; columns * page < 2^31     */
+    int64_t columns;         /* columns of table, >= 1; columns * page <= 2^30    */
     int64_t k_stride[3];     /* page, head, slot                                  */
     int64_t v_stride[3];     /* page, head, slot                                  */
     int64_t weight_stride[2]; /* page, head                                       */

@@ -23,8 +23,8 @@ HIP_FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function",
 ]
-SOURCES = ["kernels.hip", "probe.hip", "cache_kernels.hip", "attention.hip", "api.cpp",
-           "cache_api.cpp", "io.cpp"]
+SOURCES = ["kernels.hip", "probe.hip", "cache_kernels.hip", "attention.hip",
+           "attention_few.hip", "api.cpp", "cache_api.cpp", "io.cpp"]
 BIN = os.path.join(PKG, "bin")
 TOOLS = [("lssvm_train.cpp", "lssvm-train"), ("lssvm_predict.cpp", "lssvm-predict")]
 

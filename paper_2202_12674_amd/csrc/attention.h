@@ -1,0 +1,145 @@
+// What the attention kernels share: how calls are laid out over workgroups, the rows
+// of a tile, the key ranges of a split, and small vector helpers.
+#pragma once
+
+#include "cache_internal.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace lssvm {
+
+// How one call is laid out. A tile is `rows` rows of one sequence and key/value head
+// (row r is token r / group, head r % group of the group); its keys may be split over
+// `splits` workgroups, whose parts one more launch joins.
+struct AttentionPlan {
+  bool few;          // tiles of 16 rows, keys streamed through registers
+  int rows;          // rows per tile
+  int64_t tiles;     // at most so many tiles of one head
+  int splits;
+  int64_t pitch;     // stored scores per row (few rows with weights), else 0
+};
+
+struct AttentionArgs {
+  lssvm_cache c;
+  const void* q;
+  void* out;
+  Stride2 qs, os;
+  int64_t tokens;
+  int heads, group;
+  const int32_t* offsets;
+  float scale2;   // scale * log2(e): exponents are of two
+  bool causal, accumulate;
+  float* weight_out;
+  Stride2 ws;
+  AttentionPlan plan;
+  // workspace
+  float* lse;          // per row: log2 of the sum of exponentials (with weights)
+  float* part;         // splits x rows x dim: sums of one split, and
+  float2* part_ml;     // ... its maximum and sum of exponentials
+  float* scores;       // rows x pitch
+};
+
+// ------------------------------------------------------------- device -------
+
+struct Tile {
+  int s, length, n;      // sequence, its keys and rows (tokens)
+  int64_t first;         // its first token
+  int row0, rows;        // first row of the tile, rows of it that exist
+  int keys;              // keys that some row of the tile sees
+};
+
+// Keys that row r (of the sequence) sees.
+LSSVM_DEV int seen_keys(const AttentionArgs& a, const Tile& t, int r) {
+  const int k = a.causal ? t.length - t.n + r / a.group + 1 : t.length;
+  return k > 0 ? k : 0;
+}
+
+LSSVM_DEV void sequence_rows(const AttentionArgs& a, int s, int64_t* first, int* n) {
+  *first = clip(a.offsets[s], a.tokens);
+  const int64_t end = clip(a.offsets[s + 1], a.tokens);
+  *n = end > *first ? (int)(end - *first) : 0;
+}
+
+// The index-th tile over all sequences, found by a wave with a sequence per lane;
+// false behind the last. The result is uniform over the wave.
+LSSVM_DEV bool find_tile(const AttentionArgs& a, int64_t index, int rows, Tile* t) {
+  const int lane = threadIdx.x & 63;
+  int64_t before = 0;
+  for (int base = 0; base < a.c.sequences; base += 64) {
+    int64_t first = 0;
+    int n = 0;
+    if (base + lane < a.c.sequences) sequence_rows(a, base + lane, &first, &n);
+    const int64_t mine = ((int64_t)n * a.group + rows - 1) / rows;
+    int64_t to = mine;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int64_t o = __shfl_up(to, d);
+      if (lane >= d) to += o;
+    }
+    const uint64_t behind = __ballot(before + to > index);
+    if (behind) {
+      const int at = __ffsll((unsigned long long)behind) - 1;
+      const int64_t skipped = before + __shfl(to - mine, at);
+      t->s = __builtin_amdgcn_readfirstlane(base + at);
+      t->first = __shfl(first, at);
+      t->n = __builtin_amdgcn_readfirstlane(__shfl(n, at));
+      t->length = __builtin_amdgcn_readfirstlane(cache_length(a.c, t->s));
+      t->row0 = __builtin_amdgcn_readfirstlane((int)(index - skipped) * rows);
+      t->rows = min(rows, t->n * a.group - t->row0);
+      t->keys = seen_keys(a, *t, t->row0 + t->rows - 1);
+      return true;
+    }
+    before += __shfl(to, 63);
+  }
+  return false;
+}
+
+// Blocks of `block` keys per split, of which a tile uses ceil(blocks / per): short
+// sequences use fewer splits than the call has, none of fewer than `least` blocks.
+LSSVM_DEV int split_blocks(int keys, int block, int splits, int least) {
+  const int blocks = (keys + block - 1) / block;
+  return max((blocks + splits - 1) / splits, least);
+}
+
+// The larger of x in this lane and in the lanes 32 (16) apart.
+LSSVM_DEV float max_across_32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+LSSVM_DEV float max_across_16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// A word of one or two values of T with zeros where they are not finite, and a word of
+// codes for those: small numbers of which sums of up to 63 tell how many infinities of either sign and NaNs there were.
+constexpr float kCodePlus = 1.0f, kCodeMinus = 64.0f, kCodeNan = 4096.0f;
+template <typename T>
+LSSVM_DEV u32x2 take_wild(uint32_t word) {
+  typedef T tn __attribute__((ext_vector_type(4 / sizeof(T))));
+  tn x = __builtin_bit_cast(tn, word), c{};
+#pragma unroll
+  for (int i = 0; i < 4 / (int)sizeof(T); ++i) {
+    const float v = (float)x[i];
+    if (__builtin_isfinite(v)) continue;
+    c[i] = (T)(v != v ? kCodeNan : v > 0 ? kCodePlus : kCodeMinus);
+    x[i] = (T)0.0f;
+  }
+  return u32x2{__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, c)};
+}
+LSSVM_DEV float decode_wild(float sum) {
+  const int c = (int)sum;
+  const bool plus = c & 63, minus = c >> 6 & 63, nan = c >= 4096;
+  return nan || (plus && minus) ? __builtin_nanf("") : plus ? INFINITY : minus ? -INFINITY : 0.0f;
+}
+
+}  // namespace lssvm

@@ -1,119 +1,153 @@
-// Attention of new tokens over a paged cache (include/lssvm_cache.h).
-#include "cache_internal.h"
-
-#include <algorithm>
+// Attention of new tokens over a paged cache (include/lssvm_cache.h): how a call is
+// laid out, the joining of splits and the weights of few rows.
+#include "attention.h"
 
 namespace lssvm {
+
+hipError_t launch_attention_few(const AttentionArgs& a, hipStream_t stream);
+
 namespace {
 
-// One wave per row and head: 64 keys at a time, a key's score on a lane, with the
-// running maximum and sum of the softmax; then the values, four of a head on a lane.
-// Sums are fp32, exponents of two.
-constexpr int kRows = 4;   // rows a block
-template <typename T>
-__global__ void __launch_bounds__(64 * kRows) k_attention(AttentionArgs a, float* lse) {
-  __shared__ float q[kRows][256];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t t = (int64_t)blockIdx.x * kRows + wave;
-  const int h = blockIdx.y, group = a.heads / (int)a.c.heads, hk = h / group;
-  const int dim = (int)a.c.dim;
-  if (t >= a.tokens) return;
-  int s = 0;
-  while (s + 1 < a.c.sequences && a.offsets[s + 1] <= t) ++s;
-  const int64_t first = clip(a.offsets[s], a.tokens), end = clip(a.offsets[s + 1], a.tokens);
-  if (t < first || t >= end) return;
-  const int L = cache_length(a.c, s);
-  const int64_t seen = a.causal ? L - (end - first) + (t - first) + 1 : L;
-  const int keys = (int)(seen < 0 ? 0 : seen);
-  const T* qr = static_cast<const T*>(a.q) + t * a.qs.outer + h * a.qs.head;
-  for (int i = lane; i < dim; i += 64) q[wave][i] = (float)qr[i];
+constexpr int64_t kCUs = 256;
+constexpr int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 
-  float m = -INFINITY, l = 0.0f, o[4] = {0, 0, 0, 0};
-  for (int j0 = 0; j0 < keys; j0 += 64) {
-    int slot = 0;
-    const int page = j0 + lane < keys ? cache_page(a.c, s, j0 + lane, &slot) : -1;
-    float x = -INFINITY;
-    if (page >= 0) {
-      const T* k = static_cast<const T*>(a.c.k) + page * a.c.k_stride[0] + hk * a.c.k_stride[1] +
-                   slot * a.c.k_stride[2];
-      float sum = 0.0f;
-      for (int i = 0; i < dim; ++i) sum += q[wave][i] * (float)k[i];
-      x = sum * a.scale2;
-    }
-    float top = x;
-    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    const float next = fmaxf(m, top), base = next == -INFINITY ? 0.0f : next;
-    const float p = __builtin_amdgcn_exp2f(x - base), old = __builtin_amdgcn_exp2f(m - base);
-    m = next;
-    l = l * old + p;   // of this lane's keys
-    for (int i = 0; i < 4; ++i) o[i] *= old;
-    for (int jj = 0; jj < 64; ++jj) {
-      const int pj = __shfl(page, jj), sj = __shfl(slot, jj);
-      const float w = __shfl(p, jj);
-      if (pj < 0) continue;
-      const T* v = static_cast<const T*>(a.c.v) + pj * a.c.v_stride[0] + hk * a.c.v_stride[1] +
-                   sj * a.c.v_stride[2];
-      for (int i = 0; i < 4; ++i)
-        if (4 * lane + i < dim) o[i] += w * (float)v[4 * lane + i];
-    }
-  }
-  for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
-  T* y = static_cast<T*>(a.out) + t * a.os.outer + h * a.os.head;
-  for (int i = 0; i < 4; ++i)
-    if (4 * lane + i < dim) y[4 * lane + i] = (T)(l == 0.0f ? 0.0f : o[i] / l);
-  if (lse && lane == 0) lse[t * a.heads + h] = l == 0.0f ? INFINITY : m + log2f(l);
+AttentionPlan make_plan(const lssvm_cache& c, int64_t tokens, int heads, bool accumulate) {
+  AttentionPlan p{};
+  const int64_t group = heads / c.heads, most = c.columns * c.page;
+  p.few = true;
+  p.rows = 16;
+  // every sequence's last tile may be partly empty
+  p.tiles = tokens * group / p.rows + std::min(c.sequences, tokens);
+  // Splits: enough workgroups for every CU to hold eight, which also evens out
+  // sequences of different lengths, but none of fewer than 128 keys.
+  const int64_t whole = std::max<int64_t>(1, std::max(tokens * group / p.rows,
+                                                      std::min(c.sequences, tokens)) * c.heads);
+  const int64_t want = std::max<int64_t>(1, 8 * kCUs / whole);
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, (most + 127) / 128, 64}));
+  p.pitch = accumulate && p.few ? round_up(most, 32) : 0;
+  return p;
 }
 
-// One thread per key and head: the weights of all its rows, from the sums above.
+struct Carver {
+  char* base;
+  size_t off = 0;
+  template <typename U>
+  U* take(int64_t count) {
+    U* p = base ? reinterpret_cast<U*>(base + off) : nullptr;
+    off = (off + (size_t)count * sizeof(U) + 255) / 256 * 256;
+    return p;
+  }
+};
+
+size_t carve(AttentionArgs& a, void* workspace) {
+  Carver c{static_cast<char*>(workspace)};
+  const int64_t rows = a.tokens * a.heads;
+  a.lse = c.take<float>(a.accumulate ? rows : 0);
+  a.part = c.take<float>(a.plan.splits > 1 ? a.plan.splits * rows * a.c.dim : 0);
+  a.part_ml = c.take<float2>(a.plan.splits > 1 ? a.plan.splits * rows : 0);
+  a.scores = c.take<float>(a.plan.pitch * rows);
+  if (!a.accumulate) a.lse = nullptr;
+  return std::max<size_t>(c.off, 256);
+}
+
+// Joins the splits of one tile: out = sum_i 2^(m_i - m) part_i / sum_i 2^(m_i - m) l_i.
+// Four values of a row per thread.
 template <typename T>
-__global__ void __launch_bounds__(256) k_weights(AttentionArgs a, const float* lse) {
+__global__ void __launch_bounds__(256) k_attention_join(AttentionArgs a, int block, int least) {
+  Tile t;
+  if (!find_tile(a, blockIdx.x, a.plan.rows, &t)) return;
+  const int per = split_blocks(t.keys, block, a.plan.splits, least);
+  const int used = ((t.keys + block - 1) / block + per - 1) / per;
+  if (used <= 1) return;
+  const int hk = blockIdx.y, dim = (int)a.c.dim, quads = dim / 4;
+  const int64_t rows = a.tokens * a.heads;
+  for (int x = threadIdx.x; x < t.rows * quads; x += 256) {
+    const int y = x / quads, d = x % quads * 4;
+    const int tok = (t.row0 + y) / a.group, h = hk * a.group + (t.row0 + y) % a.group;
+    const int64_t at = (t.first + tok) * a.heads + h;
+    float m = -INFINITY;
+    for (int i = 0; i < used; ++i) m = fmaxf(m, a.part_ml[i * rows + at].x);
+    const float base = m == -INFINITY ? 0.0f : m;
+    f32x4 v{};
+    float l = 0.0f;
+#pragma unroll 4
+    for (int i = 0; i < used; ++i) {
+      const float2 ml = a.part_ml[i * rows + at];
+      const float f = __builtin_amdgcn_exp2f(ml.x - base);
+      l += ml.y * f;
+      v += *reinterpret_cast<const f32x4*>(a.part + (i * rows + at) * dim + d) * f;
+    }
+    const float inv = 1.0f / l;
+    Loose<T, 4> w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w.v[i] = (T)(l == 0.0f ? 0.0f : v[i] * inv);
+    *reinterpret_cast<Loose<T, 4>*>(static_cast<T*>(a.out) + (t.first + tok) * a.os.outer +
+                                    h * a.os.head + d) = w;
+    if (a.lse && d == 0) a.lse[at] = l == 0.0f ? INFINITY : m + __builtin_amdgcn_logf(l);
+  }
+}
+
+// weight_out = weight + the probabilities of few rows, from their stored scores. A
+// thread per key: rows are summed in order.
+__global__ void __launch_bounds__(256) k_weights_few(AttentionArgs a) {
+  const int s = blockIdx.z, hk = blockIdx.y;
+  const int L = cache_length(a.c, s);
   const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int hk = blockIdx.y, s = blockIdx.z, group = a.heads / (int)a.c.heads;
-  const int dim = (int)a.c.dim, L = cache_length(a.c, s);
   if (j >= L) return;
   int slot;
   const int page = cache_page(a.c, s, (int)j, &slot);
   if (page < 0) return;
-  const int64_t first = clip(a.offsets[s], a.tokens), end = clip(a.offsets[s + 1], a.tokens);
-  const T* k = static_cast<const T*>(a.c.k) + page * a.c.k_stride[0] + hk * a.c.k_stride[1] +
-               slot * a.c.k_stride[2];
+  int64_t first;
+  int n;
+  sequence_rows(a, s, &first, &n);
   float gain = 0.0f;
-  for (int64_t t = first; t < end; ++t) {
-    if (a.causal && j > L - (end - first) + (t - first)) continue;
-    for (int h = hk * group; h < (hk + 1) * group; ++h) {
-      const T* q = static_cast<const T*>(a.q) + t * a.qs.outer + h * a.qs.head;
-      float sum = 0.0f;
-      for (int i = 0; i < dim; ++i) sum += (float)q[i] * (float)k[i];
-      gain += __builtin_amdgcn_exp2f(sum * a.scale2 - lse[t * a.heads + h]);
-    }
+  for (int i = 0; i < n; ++i) {
+    if (a.causal && j > (int64_t)L - n + i) continue;
+    const int64_t row = (first + i) * a.heads + hk * a.group;
+    for (int h = 0; h < a.group; ++h)
+      gain += __builtin_amdgcn_exp2f(a.scores[(row + h) * a.plan.pitch + j] - a.lse[row + h]);
   }
   const float old = a.c.weight[page * a.c.weight_stride[0] + hk * a.c.weight_stride[1] + slot];
   a.weight_out[page * a.ws.outer + hk * a.ws.head + slot] = old + gain;
 }
 
-template <typename T>
-hipError_t launch(const AttentionArgs& a, float* lse, hipStream_t stream) {
-  if (a.tokens > 0)
-    k_attention<T><<<dim3((unsigned)((a.tokens + kRows - 1) / kRows), (unsigned)a.heads),
-                     64 * kRows, 0, stream>>>(a, a.accumulate ? lse : nullptr);
-  if (a.accumulate)
-    k_weights<T><<<dim3((unsigned)((a.c.columns * a.c.page + 255) / 256), (unsigned)a.c.heads,
-                        (unsigned)a.c.sequences),
-                   256, 0, stream>>>(a, lse);
-  return hipGetLastError();
-}
-
 }  // namespace
 
-size_t attention_workspace(const lssvm_cache&, int64_t tokens, int heads, bool accumulate) {
-  return 256 + (accumulate ? (size_t)tokens * heads * sizeof(float) : 0);
+size_t attention_workspace(const lssvm_cache& c, int64_t tokens, int heads, bool accumulate) {
+  AttentionArgs a{};
+  a.c = c;
+  a.tokens = tokens;
+  a.heads = heads;
+  a.accumulate = accumulate;
+  a.plan = make_plan(c, tokens, heads, accumulate);
+  return carve(a, nullptr);
 }
 
-hipError_t launch_attention(const AttentionArgs& a, void* workspace, hipStream_t stream) {
-  float* lse = static_cast<float*>(workspace);
-  if (a.c.dtype == LSSVM_BF16) return launch<bf16_t>(a, lse, stream);
-  if (a.c.dtype == LSSVM_F16) return launch<f16_t>(a, lse, stream);
-  return launch<float>(a, lse, stream);
+hipError_t launch_attention(AttentionArgs a, void* workspace, hipStream_t stream) {
+  a.plan = make_plan(a.c, a.tokens, a.heads, a.accumulate);
+  carve(a, workspace);
+  hipError_t e;
+  if (a.tokens > 0) {
+    if ((e = launch_attention_few(a, stream)) != hipSuccess) return e;
+    if (a.plan.splits > 1) {
+      const dim3 grid((unsigned)a.plan.tiles, (unsigned)a.c.heads);
+      const int block = a.c.dtype == LSSVM_F32 ? 16 : 32, least = 4;
+      if (a.c.dtype == LSSVM_BF16)
+        k_attention_join<bf16_t><<<grid, 256, 0, stream>>>(a, block, least);
+      else if (a.c.dtype == LSSVM_F16)
+        k_attention_join<f16_t><<<grid, 256, 0, stream>>>(a, block, least);
+      else
+        k_attention_join<float><<<grid, 256, 0, stream>>>(a, block, least);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+  }
+  if (a.accumulate) {
+    k_weights_few<<<dim3((unsigned)((a.c.columns * a.c.page + 255) / 256), (unsigned)a.c.heads,
+                         (unsigned)a.c.sequences),
+                    256, 0, stream>>>(a);
+    return hipGetLastError();
+  }
+  return hipSuccess;
 }
 
 }  // namespace lssvm

@@ -1,0 +1,446 @@
+// Attention of few rows per sequence (single tokens, and up to a few) over a paged
+// cache: include/lssvm_cache.h.
+#include "attention.h"
+
+namespace lssvm {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kLeastBlocks = kWaves;   // of a split: one per wave
+
+// The matrix cores on 16 keys x 16 rows.
+template <typename T>
+struct Mfma16;
+template <>
+struct Mfma16<bf16_t> {
+  static LSSVM_DEV f32x4 mul(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+};
+template <>
+struct Mfma16<f16_t> {
+  static LSSVM_DEV f32x4 mul(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+};
+template <>
+struct Mfma16<float> {
+  // 16 contraction places as four products of 4
+  static LSSVM_DEV f32x4 mul(u32x4 a, u32x4 b, f32x4 c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c, 0,
+                                               0, 0);
+    return c;
+  }
+};
+
+// What follows from the type and the width. Lane (m, g) = (lane % 16, lane / 16).
+// Products run over 16-byte chunks of a row: chunk 4c + g is lane group g's share of
+// step c, for keys and queries alike. Values: lane m holds CE consecutive ones of each
+// of NC parts of a row, value 16 CE part + CE m + e; keys 16b + 4g + i, which is where
+// the scores of its column stand, so that they never change lanes.
+template <typename T, int D>
+struct Shape {
+  static constexpr int VE = kVec<T>;
+  static constexpr int KB = sizeof(T) == 2 ? 2 : 1;      // blocks of 16 keys per step
+  static constexpr int KEYS = 16 * KB;
+  static constexpr int KC = D / (4 * VE);                // 16-byte chunks of a key per lane
+  static constexpr int CE = D / 16 < VE ? D / 16 : VE;   // values of a chunk
+  static constexpr int CW = CE * (int)sizeof(T) / 4;     // ... in words
+  static constexpr int NC = D / (16 * CE);
+  static constexpr int VR = 4 * KB;                      // rows of values per lane
+};
+
+// One tile of 16 rows against one split of its keys. Every wave takes 32 (fp32: 16)
+// keys at a time straight from memory into registers, scores S^T = K Q^T, keeps the
+// running maximum and sum of every row and adds O^T += V^T P^T. The values come in
+// rows and are needed in columns: 8 x 8 of them are transposed by byte permutes, in
+// fp32 the operand is a row already. Probabilities enter the 16-bit product as two
+// 16-bit parts, since the matrix cores have the time (the kernel waits for memory).
+// The waves' sums are joined in LDS.
+//
+// Keys of the next step are loaded as soon as the scores are formed, values as soon
+// as the product is issued, so that a wave has loads in flight all the time. BLOCKS:
+// the pages hold whole runs of 16 keys, whose page is then looked up once.
+template <typename T, int D, bool BLOCKS>
+__global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) {
+  using S = Shape<T, D>;
+  constexpr int VE = S::VE, KB = S::KB, KEYS = S::KEYS, KC = S::KC, CE = S::CE, CW = S::CW,
+                NC = S::NC, VR = S::VR;
+  constexpr bool HALF = sizeof(T) == 2;
+  __shared__ float sum_o[kWaves][16][D];
+  __shared__ float sum_m[kWaves][16], sum_l[kWaves][16];
+
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int split = blockIdx.y, hk = blockIdx.z;
+  Tile t;
+  if (!find_tile(a, blockIdx.x, 16, &t)) return;
+  const int per = split_blocks(t.keys, KEYS, a.plan.splits, kLeastBlocks);
+  const int blocks = (t.keys + KEYS - 1) / KEYS;
+  const int used = max(1, (blocks + per - 1) / per);
+  if (split >= used) return;
+  const int block0 = split * per, block1 = min(blocks, block0 + per);
+  const int dim = (int)a.c.dim;
+
+  // this lane's row, its queries and the keys it sees
+  const int r = t.row0 + min(m, t.rows - 1);
+  const int token = r / a.group, head = hk * a.group + r % a.group;
+  const int64_t row = (t.first + token) * a.heads + head;
+  const int lim = m < t.rows ? seen_keys(a, t, r) : 0;
+  const int all_see = seen_keys(a, t, t.row0);   // keys that every row sees
+  u32x4 qf[KC];
+  {
+    const T* q = static_cast<const T*>(a.q) + (t.first + token) * a.qs.outer + head * a.qs.head;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      const int at = (4 * c + g) * VE;
+      qf[c] = u32x4{};
+      if (at < dim)
+        qf[c] = __builtin_bit_cast(u32x4, *reinterpret_cast<const Loose<T, VE>*>(q + at));
+    }
+  }
+
+  const T* kbase = static_cast<const T*>(a.c.k) + hk * a.c.k_stride[1];
+  const T* vbase = static_cast<const T*>(a.c.v) + hk * a.c.v_stride[1];
+  const int ks = (int)a.c.k_stride[2], vs = (int)a.c.v_stride[2];
+
+  // where the keys of a step are: page (or -1) and slot; of every 16 keys, or of
+  // this lane's key
+  struct Place {
+    int page[BLOCKS ? KB : 1], slot[BLOCKS ? KB : 1];
+  };
+  auto locate = [&](int block) {
+    Place p;
+    if constexpr (BLOCKS) {
+#pragma unroll
+      for (int b = 0; b < KB; ++b) {
+        const int j = block * KEYS + 16 * b;
+        p.page[b] = -1, p.slot[b] = 0;
+        if (j < t.length) {
+          p.page[b] = cache_page(a.c, t.s, j, &p.slot[b]);
+        }
+      }
+    } else {
+      const int j = block * KEYS + (lane & (KEYS - 1));
+      p.page[0] = -1, p.slot[0] = 0;
+      if (j < t.length) p.page[0] = cache_page(a.c, t.s, j, &p.slot[0]);
+    }
+    return p;
+  };
+  u32x4 kf[KB][KC];
+  auto load_keys = [&](const Place& p) {
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+      const T* k;
+      if constexpr (BLOCKS) {
+        k = kbase + (int64_t)max(p.page[b], 0) * a.c.k_stride[0] + (int64_t)p.slot[b] * ks;
+        k += m * ks + g * VE;
+      } else {
+        const int page = __shfl(p.page[0], 16 * b + m), slot = __shfl(p.slot[0], 16 * b + m);
+        k = kbase + (int64_t)max(page, 0) * a.c.k_stride[0] + (int64_t)slot * ks + g * VE;
+      }
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        kf[b][c] = u32x4{};
+        if ((4 * c + 3) * VE < dim || (4 * c + g) * VE < dim)
+          kf[b][c] = *reinterpret_cast<const u32x4*>(k + 4 * c * VE);
+      }
+    }
+  };
+  uint32_t vf[VR][NC][CW];
+  auto load_values = [&](const Place& p) {
+#pragma unroll
+    for (int y = 0; y < VR; ++y) {
+      const int b = y / 4, i = y % 4;
+      const T* v;
+      if constexpr (BLOCKS) {
+        v = vbase + (int64_t)max(p.page[b], 0) * a.c.v_stride[0] + (int64_t)p.slot[b] * vs;
+        v += (4 * g + i) * vs + CE * m;
+      } else {
+        const int from = 16 * b + 4 * g + i;
+        const int page = __shfl(p.page[0], from), slot = __shfl(p.slot[0], from);
+        v = vbase + (int64_t)max(page, 0) * a.c.v_stride[0] + (int64_t)slot * vs + CE * m;
+      }
+#pragma unroll
+      for (int part = 0; part < NC; ++part) {
+        const int at = 16 * CE * part;
+        if (at + CE * m < dim) {
+          if constexpr (CW == 4) {
+            const u32x4 w = *reinterpret_cast<const u32x4*>(v + at);
+#pragma unroll
+            for (int i2 = 0; i2 < 4; ++i2) vf[y][part][i2] = w[i2];
+          } else {
+            const u32x2 w = *reinterpret_cast<const u32x2*>(v + at);
+            vf[y][part][0] = w[0], vf[y][part][1] = w[1];
+          }
+        } else {
+#pragma unroll
+          for (int i2 = 0; i2 < CW; ++i2) vf[y][part][i2] = 0;
+        }
+      }
+    }
+  };
+
+  f32x4 o[NC * CE];
+  float top, l;
+
+  // O^T += V^T p for the step's values: `hi` and `lo` are the 16-bit parts of p, in fp32
+  // p itself. WILD: values that are not finite are left out of that, and enter as
+  // codes times whether the row sees the key, `see` (as a vector of T, or fp32).
+  auto add_values = [&](auto with_wild, u32x4 hi, u32x4 lo, u32x4 see, f32x4 p) {
+    constexpr bool WILD = decltype(with_wild)::value;
+#pragma unroll
+    for (int part = 0; part < NC; ++part)
+#pragma unroll
+      for (int e = 0; e < CE; ++e) {
+        f32x4& acc = o[part * CE + e];
+        u32x4 v;
+        if constexpr (HALF) {
+          const uint32_t pick = e & 1 ? 0x07060302u : 0x05040100u;
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            v[u] = __builtin_amdgcn_perm(vf[2 * u + 1][part][e / 2], vf[2 * u][part][e / 2], pick);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = vf[i][part][e];
+        }
+        if constexpr (WILD) {
+          u32x4 code;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const u32x2 taken = take_wild<T>(v[u]);
+            v[u] = taken[0], code[u] = taken[1];
+          }
+          f32x4 sum{};
+          if constexpr (HALF) {
+            sum = Mfma16<T>::mul(code, see, sum);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              sum = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(code[i]),
+                                                         __uint_as_float(see[i]), sum, 0, 0, 0);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[i] += decode_wild(sum[i]);
+        }
+        if constexpr (HALF) {
+          acc = Mfma16<T>::mul(v, hi, acc);
+          acc = Mfma16<T>::mul(v, lo, acc);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[i]), p[i], acc, 0, 0, 0);
+        }
+      }
+  };
+
+  auto sweep = [&](auto with_wild) {
+#pragma unroll
+    for (int e = 0; e < NC * CE; ++e) o[e] = f32x4{};
+    top = -INFINITY, l = 0.0f;
+    int block = block0 + wave;
+    Place now = locate(min(block, max(blocks - 1, 0)));
+    if (block < block1) load_keys(now), load_values(now);
+    Place next = locate(block + kWaves);
+    for (; block < block1; block += kWaves) {
+      const int j0 = block * KEYS;
+      f32x4 s[KB];
+#pragma unroll
+      for (int b = 0; b < KB; ++b) {
+        s[b] = f32x4{};
+#pragma unroll
+        for (int c = 0; c < KC; ++c) s[b] = Mfma16<T>::mul(kf[b][c], qf[c], s[b]);
+      }
+      // holes, by key of this lane (bit 4b + i), or none
+      bool whole = true;
+      uint32_t there = 0xFFu;
+      if constexpr (BLOCKS) {
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+          if (now.page[b] < 0) there &= ~(0xFu << (4 * b)), whole = false;
+      } else {
+        const uint64_t ok = __ballot(now.page[0] >= 0);
+        whole = ok == ~(uint64_t)0;
+        there = (uint32_t)(ok >> (4 * g)) & 0xFu;
+        if constexpr (KB == 2) there |= ((uint32_t)(ok >> (16 + 4 * g)) & 0xFu) << 4;
+      }
+      if (block + kWaves < block1) load_keys(next);
+
+      const bool masked = !whole || j0 + KEYS > all_see;
+#pragma unroll
+      for (int b = 0; b < KB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[b][i] *= a.scale2;
+      if (masked) {
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (j0 + 16 * b + 4 * g + i >= lim || !(there >> (4 * b + i) & 1)) s[b][i] = -INFINITY;
+      }
+      if (a.plan.pitch && m < t.rows) {
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+          *reinterpret_cast<f32x4*>(a.scores + row * a.plan.pitch + j0 + 16 * b + 4 * g) = s[b];
+      }
+      float high = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
+      if constexpr (KB == 2)
+        high = fmaxf(high, fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+      high = max_across_32(max_across_16(high));
+      if (__any(high > top)) {
+        const float grown = fmaxf(top, high);
+        const float old = __builtin_amdgcn_exp2f(top - (grown == -INFINITY ? 0.0f : grown));
+        top = grown;
+        l *= old;
+#pragma unroll
+        for (int e = 0; e < NC * CE; ++e) o[e] *= old;
+      }
+      const float base = top == -INFINITY ? 0.0f : top;
+      f32x4 p[KB];
+#pragma unroll
+      for (int b = 0; b < KB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[b][i] = __builtin_amdgcn_exp2f(s[b][i] - base);
+          l += p[b][i];
+        }
+      u32x4 hi{}, lo{};
+      if constexpr (HALF) {
+        typedef T t8 __attribute__((ext_vector_type(8)));
+        t8 h, d;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          h[i] = (T)p[i / 4][i % 4];
+          d[i] = (T)(p[i / 4][i % 4] - (float)h[i]);
+        }
+        hi = __builtin_bit_cast(u32x4, h);
+        lo = __builtin_bit_cast(u32x4, d);
+      }
+
+      // values of keys that are not there are left out, whatever they are
+      if (masked) {
+#pragma unroll
+        for (int y = 0; y < VR; ++y) {
+          const bool in = j0 + 16 * (y / 4) + 4 * g + y % 4 < t.length && (there >> y & 1);
+#pragma unroll
+          for (int part = 0; part < NC; ++part)
+#pragma unroll
+            for (int w = 0; w < CW; ++w)
+              if (!in) vf[y][part][w] = 0;
+        }
+      }
+      if constexpr (decltype(with_wild)::value) {
+        u32x4 see;
+        if constexpr (HALF) {
+          typedef T t8 __attribute__((ext_vector_type(8)));
+          t8 h;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) h[i] = s[i / 4][i % 4] == -INFINITY ? (T)0.0f : (T)1.0f;
+          see = __builtin_bit_cast(u32x4, h);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) see[i] = s[0][i] == -INFINITY ? 0 : __float_as_uint(1.0f);
+        }
+        add_values(with_wild, hi, lo, see, p[0]);
+      } else {
+        add_values(with_wild, hi, lo, u32x4{}, p[0]);
+      }
+      if (block + kWaves < block1) load_values(next);
+      now = next;
+      next = locate(block + 2 * kWaves);
+    }
+  };
+  // A value that is not finite makes its product with any probability so, zeros of rows
+  // that do not see it among them: then the wave's keys are gone over once more, with
+  // such values apart.
+  sweep(std::false_type{});
+  bool finite = true;
+#pragma unroll
+  for (int e = 0; e < NC * CE; ++e)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) finite &= __builtin_isfinite(o[e][i]);
+  if (__any(!finite)) sweep(std::true_type{});
+
+  // join the waves' sums
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  if (g == 0) sum_m[wave][m] = top, sum_l[wave][m] = l;
+  __syncthreads();
+  float most = sum_m[0][m];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) most = fmaxf(most, sum_m[w][m]);
+  const float base = most == -INFINITY ? 0.0f : most;
+  const float mine = __builtin_amdgcn_exp2f(top - base);
+  if (m < t.rows) {
+#pragma unroll
+    for (int part = 0; part < NC; ++part)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < CE; ++e)
+          sum_o[wave][m][16 * CE * part + CE * (4 * g + i) + e] = o[part * CE + e][i] * mine;
+  }
+  __syncthreads();
+  const bool last = used == 1;
+  const int64_t rows = a.tokens * a.heads;
+  for (int x = threadIdx.x; x < t.rows * (D / 4); x += 64 * kWaves) {
+    const int y = x / (D / 4), d = x % (D / 4) * 4;
+    if (d >= dim) continue;
+    f32x4 v = *reinterpret_cast<const f32x4*>(&sum_o[0][y][d]);
+    float high = sum_m[0][y];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) {
+      v += *reinterpret_cast<const f32x4*>(&sum_o[w][y][d]);
+      high = fmaxf(high, sum_m[w][y]);
+    }
+    float total = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+      total += sum_l[w][y] * __builtin_amdgcn_exp2f(sum_m[w][y] - (high == -INFINITY ? 0.0f : high));
+    const int tok = (t.row0 + y) / a.group, h = hk * a.group + (t.row0 + y) % a.group;
+    const int64_t at = (t.first + tok) * a.heads + h;
+    if (last) {
+      const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+      T* out = static_cast<T*>(a.out) + (t.first + tok) * a.os.outer + h * a.os.head + d;
+      Loose<T, 4> w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w.v[i] = (T)(total == 0.0f ? 0.0f : v[i] * inv);
+      *reinterpret_cast<Loose<T, 4>*>(out) = w;
+      if (a.lse && d == 0) a.lse[at] = total == 0.0f ? INFINITY : high + __builtin_amdgcn_logf(total);
+    } else {
+      *reinterpret_cast<f32x4*>(a.part + (split * rows + at) * dim + d) = v;
+      if (d == 0) a.part_ml[split * rows + at] = float2{high, total};
+    }
+  }
+}
+
+template <typename T, int D>
+hipError_t launch_width(const AttentionArgs& a, hipStream_t stream) {
+  const dim3 grid((unsigned)a.plan.tiles, (unsigned)a.plan.splits, (unsigned)a.c.heads);
+  if (a.c.page % 16 == 0)
+    k_attention_few<T, D, true><<<grid, 64 * kWaves, 0, stream>>>(a);
+  else
+    k_attention_few<T, D, false><<<grid, 64 * kWaves, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_type(const AttentionArgs& a, hipStream_t stream) {
+  if (a.c.dim <= 64) return launch_width<T, 64>(a, stream);
+  if (a.c.dim <= 128) return launch_width<T, 128>(a, stream);
+  return launch_width<T, 256>(a, stream);
+}
+
+}  // namespace
+
+hipError_t launch_attention_few(const AttentionArgs& a, hipStream_t stream) {
+  if (a.c.dtype == LSSVM_BF16) return launch_type<bf16_t>(a, stream);
+  if (a.c.dtype == LSSVM_F16) return launch_type<f16_t>(a, stream);
+  return launch_type<float>(a, stream);
+}
+
+}  // namespace lssvm

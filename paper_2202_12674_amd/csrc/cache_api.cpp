@@ -1,5 +1,5 @@
 // Host side of include/lssvm_cache.h: argument checks and launches.
-#include "cache_internal.h"
+#include "attention.h"
 #include "lssvm_error.h"
 
 #include <algorithm>
@@ -10,6 +10,8 @@ namespace {
 
 constexpr int64_t kMaxHeads = 65535;
 constexpr int64_t kMaxTokens = (int64_t(1) << 31) - 1;
+constexpr int64_t kMaxKeys = int64_t(1) << 30;      // of a sequence
+constexpr int64_t kMaxSlotStride = int64_t(1) << 26;
 constexpr int64_t kMaxStride = int64_t(1) << 40;
 
 #define CACHE_TRY(expr)              \
@@ -63,14 +65,15 @@ int check_cache(const lssvm_cache* c) {
   if (c->pages < 1 || c->pages > kMaxTokens || c->heads < 1 || c->heads > kMaxHeads ||
       c->page < 1 || c->page > kMaxTokens || c->sequences < 1 || c->sequences > kMaxHeads)
     return bad("cache: pages, heads, page or sequences out of range");
-  if (c->columns < 1 || c->columns > kMaxTokens || c->columns * c->page > kMaxTokens)
-    return bad("cache: columns * page must be 1 .. 2^31 - 1");
+  if (c->columns < 1 || c->columns > kMaxTokens || c->columns * c->page > kMaxKeys)
+    return bad("cache: columns * page must be 1 .. 2^30");
   if (c->table_stride < c->columns && c->sequences > 1)
     return bad("cache: table_stride must be at least columns");
   if (!aligned(c->k, 16) || !aligned(c->v, 16)) return bad("cache: k and v must be 16-byte aligned");
   const int64_t count[3] = {c->pages, c->heads, c->page};
   for (const int64_t* st : {c->k_stride, c->v_stride}) {
-    if (!strides_in_range(st, 3)) return bad("cache: a stride out of range");
+    if (!strides_in_range(st, 3) || (c->page > 1 && st[2] > kMaxSlotStride))
+      return bad("cache: a stride out of range");
     for (int i = 0; i < 3; ++i)
       if (count[i] > 1 && st[i] * element(c->dtype) % 16)
         return bad("cache: rows of k and v must begin on 16 bytes");
@@ -283,6 +286,7 @@ int lssvm_attention(const lssvm_cache* cache, const void* q, const int64_t* q_st
   a.out = out;
   a.tokens = tokens;
   a.heads = (int)heads;
+  a.group = (int)(heads / cache->heads);
   a.offsets = offsets;
   a.scale2 = (float)(scale * 1.4426950408889634074);
   a.causal = causal != 0;

@@ -35,21 +35,9 @@ struct AppendArgs {
 };
 hipError_t launch_append(const AppendArgs& a, hipStream_t stream);
 
-struct AttentionArgs {
-  lssvm_cache c;
-  const void* q;
-  void* out;
-  Stride2 qs, os;
-  int64_t tokens;
-  int heads;
-  const int32_t* offsets;
-  float scale2;   // scale * log2(e): exponents are of two
-  bool causal, accumulate;
-  float* weight_out;
-  Stride2 ws;
-};
+struct AttentionArgs;   // attention.h
 size_t attention_workspace(const lssvm_cache& c, int64_t tokens, int heads, bool accumulate);
-hipError_t launch_attention(const AttentionArgs& a, void* workspace, hipStream_t stream);
+hipError_t launch_attention(AttentionArgs a, void* workspace, hipStream_t stream);
 
 struct EvictArgs {
   lssvm_cache from, to;

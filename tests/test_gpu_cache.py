@@ -14,11 +14,15 @@ def _t(torch, name):
     return {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}[name]
 
 
+def torch_equal(a, b):
+    return bool(((a == b) | (a.isnan() & b.isnan())).all())
+
+
 def _check(got, want, bound, what=""):
     """got within bound of want; equal infinities and NaNs where want has them."""
     got = got.double().cpu()
     fine = want.isfinite()
-    assert bool((got.isfinite() == fine).all()), what
+    assert torch_equal(got[~fine], want[~fine]), what
     worst = float(((got - want).abs() - bound)[fine].max()) if bool(fine.any()) else 0.0
     assert worst <= 0.0, what
 
@@ -149,13 +153,17 @@ def offsets_of(torch, new):
 
 
 def run_attention(torch_dev, dtype, lengths, new, hq, hkv, d, page, causal=True, accumulate=False,
-                  layout="heads", holes=0, behind=0, scale=None, seed=1, split_q=False, big=1.0):
+                  layout="heads", holes=0, behind=0, scale=None, seed=1, split_q=False, big=1.0,
+                  wild=()):
     torch, dev = torch_dev
     import cache_oracle as O
     import paper_2202_12674_amd as P
     cache, (k, v, table, lens, w) = make(torch, dev, dtype, lengths, hkv, d, page, seed, layout,
                                          holes=holes)
     g = torch.Generator().manual_seed(seed + 1)
+    for s, j, h, x, value in wild:     # values (x of head h of key j) that are not finite
+        v[int(table[s, j // page]), h, j % page, x] = value
+    cache.v.copy_(v)
     tokens = sum(new) + behind
     q = (big * torch.randn(tokens, hq, d, generator=g)).to(k.dtype)
     off = offsets_of(torch, new)
@@ -172,7 +180,7 @@ def run_attention(torch_dev, dtype, lengths, new, hq, hkv, d, page, causal=True,
     want, bound, ww, slack = O.attention(q, k, v, table, lens, off,
                                          d ** -0.5 if scale is None else scale, causal,
                                          w if accumulate else None)
-    there = bound >= 0
+    there = bound != -1
     _check(y[there.to(dev)], want[there], bound[there], "out")
     assert bool((y.cpu()[~there] == 3.0).all())
     if accumulate:
@@ -244,6 +252,19 @@ def test_attention_holes_and_rows_behind_the_last_sequence(torch_dev, dtype, new
 def test_attention_scales(torch_dev, dtype, scale):
     run_attention(torch_dev, dtype, [99, 260], [1, 1], 4, 2, 64, 16, True, True, scale=scale)
     run_attention(torch_dev, dtype, [99, 260], [80, 100], 4, 2, 64, 16, True, True, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("new", [5, 60, 200])
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 21), (256, 32)])
+def test_values_that_are_not_finite_reach_only_rows_that_see_them(torch_dev, dtype, new, d, page):
+    """Infinities and NaNs in the values of new tokens, one the first, one the last of a
+    chunk: rows before them must not change, rows from them on take them over."""
+    wild = [(0, 299, 0, 3, math.inf), (0, 299, 0, 4, math.nan), (0, 298, 0, 3, -math.inf),
+            (0, 300 - new, 1, d - 1, math.inf), (0, 300 - new // 2, 0, 0, -math.inf),
+            (1, 130 - new // 2 if new < 130 else 70, 1, 5, math.inf)]
+    run_attention(torch_dev, dtype, [300, 130], [new, min(new, 130)], 4, 2, d, page, True, True,
+                  wild=wild)
 
 
 def test_attention_of_large_scores(torch_dev):
