@@ -24,7 +24,8 @@ HIP_FLAGS = [
     "-Wall", "-Wno-unused-function",
 ]
 SOURCES = ["kernels.hip", "probe.hip", "cache_kernels.hip", "attention.hip",
-           "attention_few.hip", "api.cpp", "cache_api.cpp", "io.cpp"]
+           "attention_few.hip", "attention_chunk.hip", "api.cpp",
+           "cache_api.cpp", "io.cpp"]
 BIN = os.path.join(PKG, "bin")
 TOOLS = [("lssvm_train.cpp", "lssvm-train"), ("lssvm_predict.cpp", "lssvm-predict")]
 

@@ -40,6 +40,14 @@ struct AttentionArgs {
   float* scores;       // rows x pitch
 };
 
+// Keys per step of either kernel, and the fewest steps of a split.
+template <typename T>
+constexpr int few_keys = sizeof(T) == 2 ? 32 : 16;
+template <typename T>
+constexpr int chunk_keys = sizeof(T) == 2 ? 64 : 32;
+constexpr int kFewLeast = 4, kChunkLeast = 4;
+constexpr int kChunkRB = 1;   // blocks of 32 rows per wave
+
 // ------------------------------------------------------------- device -------
 
 struct Tile {
@@ -121,7 +129,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // A word of one or two values of T with zeros where they are not finite, and a word of
-// codes for those: small numbers of which sums of up to 63 tell how many infinities of either sign and NaNs there were.
+// codes for those: small numbers of which sums of up to 63 tell how many infinities of
+// either sign and NaNs there were.
 constexpr float kCodePlus = 1.0f, kCodeMinus = 64.0f, kCodeNan = 4096.0f;
 template <typename T>
 LSSVM_DEV u32x2 take_wild(uint32_t word) {

@@ -5,6 +5,8 @@
 namespace lssvm {
 
 hipError_t launch_attention_few(const AttentionArgs& a, hipStream_t stream);
+hipError_t launch_attention_chunk(const AttentionArgs& a, hipStream_t stream);
+hipError_t launch_weights_chunk(const AttentionArgs& a, hipStream_t stream);
 
 namespace {
 
@@ -14,16 +16,17 @@ constexpr int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 AttentionPlan make_plan(const lssvm_cache& c, int64_t tokens, int heads, bool accumulate) {
   AttentionPlan p{};
   const int64_t group = heads / c.heads, most = c.columns * c.page;
-  p.few = true;
-  p.rows = 16;
+  p.few = tokens * group <= 32 * c.sequences;
+  p.rows = p.few ? 16 : 128 * kChunkRB;
   // every sequence's last tile may be partly empty
   p.tiles = tokens * group / p.rows + std::min(c.sequences, tokens);
   // Splits: enough workgroups for every CU to hold eight, which also evens out
   // sequences of different lengths, but none of fewer than 128 keys.
   const int64_t whole = std::max<int64_t>(1, std::max(tokens * group / p.rows,
                                                       std::min(c.sequences, tokens)) * c.heads);
-  const int64_t want = std::max<int64_t>(1, 8 * kCUs / whole);
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, (most + 127) / 128, 64}));
+  const int64_t want = std::max<int64_t>(1, (p.few ? 8 : 2) * kCUs / whole);
+  p.splits = (int)std::max<int64_t>(
+      1, std::min<int64_t>({want, (most + 127) / 128, p.few ? 64 : 16}));
   p.pitch = accumulate && p.few ? round_up(most, 32) : 0;
   return p;
 }
@@ -123,31 +126,31 @@ size_t attention_workspace(const lssvm_cache& c, int64_t tokens, int heads, bool
   return carve(a, nullptr);
 }
 
+template <typename T>
+hipError_t join(const AttentionArgs& a, hipStream_t stream) {
+  const dim3 grid((unsigned)a.plan.tiles, (unsigned)a.c.heads);
+  const int block = a.plan.few ? few_keys<T> : chunk_keys<T>;
+  k_attention_join<T><<<grid, 256, 0, stream>>>(a, block, a.plan.few ? kFewLeast : kChunkLeast);
+  return hipGetLastError();
+}
+
 hipError_t launch_attention(AttentionArgs a, void* workspace, hipStream_t stream) {
   a.plan = make_plan(a.c, a.tokens, a.heads, a.accumulate);
   carve(a, workspace);
-  hipError_t e;
+  hipError_t e = hipSuccess;
   if (a.tokens > 0) {
-    if ((e = launch_attention_few(a, stream)) != hipSuccess) return e;
-    if (a.plan.splits > 1) {
-      const dim3 grid((unsigned)a.plan.tiles, (unsigned)a.c.heads);
-      const int block = a.c.dtype == LSSVM_F32 ? 16 : 32, least = 4;
-      if (a.c.dtype == LSSVM_BF16)
-        k_attention_join<bf16_t><<<grid, 256, 0, stream>>>(a, block, least);
-      else if (a.c.dtype == LSSVM_F16)
-        k_attention_join<f16_t><<<grid, 256, 0, stream>>>(a, block, least);
-      else
-        k_attention_join<float><<<grid, 256, 0, stream>>>(a, block, least);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
+    e = a.plan.few ? launch_attention_few(a, stream) : launch_attention_chunk(a, stream);
+    if (e == hipSuccess && a.plan.splits > 1)
+      e = a.c.dtype == LSSVM_BF16  ? join<bf16_t>(a, stream)
+          : a.c.dtype == LSSVM_F16 ? join<f16_t>(a, stream)
+                                   : join<float>(a, stream);
   }
-  if (a.accumulate) {
-    k_weights_few<<<dim3((unsigned)((a.c.columns * a.c.page + 255) / 256), (unsigned)a.c.heads,
-                         (unsigned)a.c.sequences),
-                    256, 0, stream>>>(a);
-    return hipGetLastError();
-  }
-  return hipSuccess;
+  if (e != hipSuccess || !a.accumulate) return e;
+  if (!a.plan.few) return launch_weights_chunk(a, stream);
+  k_weights_few<<<dim3((unsigned)((a.c.columns * a.c.page + 255) / 256), (unsigned)a.c.heads,
+                       (unsigned)a.c.sequences),
+                  256, 0, stream>>>(a);
+  return hipGetLastError();
 }
 
 }  // namespace lssvm

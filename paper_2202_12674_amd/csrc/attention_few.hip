@@ -6,7 +6,6 @@ namespace lssvm {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kLeastBlocks = kWaves;   // of a split: one per wave
 
 // The matrix cores on 16 keys x 16 rows.
 template <typename T>
@@ -45,8 +44,8 @@ struct Mfma16<float> {
 template <typename T, int D>
 struct Shape {
   static constexpr int VE = kVec<T>;
-  static constexpr int KB = sizeof(T) == 2 ? 2 : 1;      // blocks of 16 keys per step
-  static constexpr int KEYS = 16 * KB;
+  static constexpr int KEYS = few_keys<T>;               // of a step
+  static constexpr int KB = KEYS / 16;                   // ... blocks of 16
   static constexpr int KC = D / (4 * VE);                // 16-byte chunks of a key per lane
   static constexpr int CE = D / 16 < VE ? D / 16 : VE;   // values of a chunk
   static constexpr int CW = CE * (int)sizeof(T) / 4;     // ... in words
@@ -79,7 +78,7 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
   const int split = blockIdx.y, hk = blockIdx.z;
   Tile t;
   if (!find_tile(a, blockIdx.x, 16, &t)) return;
-  const int per = split_blocks(t.keys, KEYS, a.plan.splits, kLeastBlocks);
+  const int per = split_blocks(t.keys, KEYS, a.plan.splits, kFewLeast);
   const int blocks = (t.keys + KEYS - 1) / KEYS;
   const int used = max(1, (blocks + per - 1) / per);
   if (split >= used) return;
