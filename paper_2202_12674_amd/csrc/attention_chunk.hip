@@ -9,8 +9,6 @@ constexpr int kWaves = 4;
 
 typedef __attribute__((address_space(1))) void* gptr_t;
 typedef __attribute__((address_space(3))) void* lptr_t;
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) s16x4* l16x4_t;
 
 // 32 x 32 products over two 16-byte chunks: lane l has chunk l / 32 of row l % 32 of
 // either operand.
@@ -37,6 +35,23 @@ LSSVM_DEV constexpr int result_row(int i, int h) { return 8 * (i / 4) + 4 * h + 
 template <typename T>
 LSSVM_DEV u32x4 load_loose(const T* p) {
   return __builtin_bit_cast(u32x4, *reinterpret_cast<const Loose<T, kVec<T>>*>(p));
+}
+
+// use(n, read(n)) for n < N, with the reads (of LDS) four ahead, in just this order: left
+// alone, the compiler waits for every read.
+template <int N, typename R, typename U>
+LSSVM_DEV void read_ahead(R read, U use) {
+  constexpr int AHEAD = N < 4 ? N : 4;
+  decltype(read(0)) f[AHEAD];
+#pragma unroll
+  for (int n = 0; n < AHEAD; ++n) f[n] = read(n);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    __builtin_amdgcn_sched_barrier(0);
+    use(n, f[n % AHEAD]);
+    if (n + AHEAD < N) f[n % AHEAD] = read(n + AHEAD);
+  }
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 // Kinds of values, and the values of a word that are of one: finite ones as they are,
@@ -80,20 +95,29 @@ struct Chunk {
   static constexpr int KC = D / (2 * VE);                        // chunks of a row per lane
   static constexpr int DB = D / 32;
   static constexpr int LOADS = KEYS * CH / (64 * kWaves);        // chunks per thread and tile
+  // rows that a thread moves are NEXT apart, at one chunk under the swizzle
+  static constexpr int NEXT = 64 * kWaves / CH, TURN = NEXT < 8 ? NEXT - 1 : 7;
+  // 16-bit values, in columns: every column's keys in 128 bytes
+  static constexpr bool HALF = sizeof(T) == 2;
+  static constexpr int VBYTES = HALF ? D * 2 * KEYS : KEYS * ROW;
+  static constexpr int VUNITS = KEYS / 4 * (D / VE);             // 4 keys x 16 bytes
+  static constexpr int VU = (VUNITS + 64 * kWaves - 1) / (64 * kWaves);
 };
 
-// Where a chunk of a row stands in LDS. Reads of keys go down 32 rows at one chunk,
-// and 8 rows in a row are spread over the banks. Reads of values take 32 bytes of four
-// rows at a time, which are kept on different banks.
-LSSVM_DEV int key_place(int row, int chunk) { return chunk ^ (row & 7); }
-LSSVM_DEV int value_place(int row, int chunk) { return chunk ^ (2 * (row & 3)); }
+// Chunks of a row (keys, and fp32 values) stand in LDS at chunk ^ (row & TURN): reads of
+// keys go down the rows at one chunk, and 8 rows in a row are spread over the banks.
+// 16-bit values in columns: 8 keys of column d, of its 8 times as many, start here. Reads
+// go down 32 columns, writes down every eighth.
+LSSVM_DEV int column_at(int d, int keys8) { return d * 128 + 16 * (keys8 ^ ((d ^ (d >> 3)) & 7)); }
 
 // One tile of 128 RB rows against one split of its keys. A step's keys and values go
 // from memory into LDS past the registers, one step ahead, and every wave takes 32 RB
 // rows over them: scores S^T = K Q^T, so that a row's scores are a lane's (and the
 // lane's 32 away); the running maximum and sum; and O^T += V^T P^T, whose operand P^T
 // the scores already are, register for register, if V^T's keys are taken in the same
-// order. V^T comes out of LDS by transposing reads, in fp32 by plain ones.
+// order. 16-bit values pass through registers on their way to LDS and are transposed
+// there once, 4 keys x 8 values per thread, so that a lane reads 8 keys of its column
+// in one piece; fp32 ones are read singly and stay in rows.
 // 16-bit types: p is rounded to the stored type for the product, half a step of it,
 // as the values themselves were; its sum is taken before that.
 template <typename T, int D, int RB>
@@ -101,10 +125,10 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
     k_attention_chunk(AttentionArgs a) {
   using S = Chunk<T, D>;
   constexpr int VE = S::VE, KEYS = S::KEYS, NB = S::NB, ROW = S::ROW, CH = S::CH, KC = S::KC,
-                DB = S::DB, LOADS = S::LOADS;
-  constexpr bool HALF = sizeof(T) == 2;
+                DB = S::DB, LOADS = S::LOADS, VU = S::VU;
+  constexpr bool HALF = S::HALF;
   __shared__ __attribute__((aligned(16))) char kt[2][KEYS * ROW];
-  __shared__ __attribute__((aligned(16))) char vt[2][KEYS * ROW];
+  __shared__ __attribute__((aligned(16))) char vt[2][S::VBYTES];
   __shared__ int64_t key_at[4][KEYS], value_at[4][KEYS];   // rows of a step, -1: none
   __shared__ uint64_t there[4];
 
@@ -126,7 +150,12 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
   const int block0 = split * per, block1 = min(blocks, block0 + per);
   const int dim = (int)a.c.dim, chunks = dim / VE;
 
-  // this lane's rows
+  // this lane's rows. Queries carry the sign of the scale (none if it is 0), so that
+  // the largest score is the largest product.
+  const float scale2 = a.scale2 == 0.0f ? 1.0f : fabsf(a.scale2);
+  const uint32_t sign = a.scale2 < 0.0f ? (HALF ? 0x80008000u : 0x80000000u) : 0;
+  const uint32_t keep = a.scale2 == 0.0f ? 0 : ~0u;
+  auto turned = [&](u32x4 q) { return (q ^ sign) & keep; };
   u32x4 qf[RB][KC];
   int lim[RB];
   int all_see = t.length, some_see = 0;   // keys that every (any) row of the wave sees
@@ -138,7 +167,7 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
     const T* q = static_cast<const T*>(a.q) + (t.first + tok) * a.qs.outer + head * a.qs.head;
 #pragma unroll
     for (int k = 0; k < KC; ++k)
-      qf[rb][k] = 2 * k + h < chunks ? load_loose(q + (2 * k + h) * VE) : u32x4{};
+      qf[rb][k] = 2 * k + h < chunks ? turned(load_loose(q + (2 * k + h) * VE)) : u32x4{};
   }
   {
     const int y = wave * 32 * RB;
@@ -150,6 +179,14 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
 
   const T* kbase = static_cast<const T*>(a.c.k) + hk * a.c.k_stride[1];
   const T* vbase = static_cast<const T*>(a.c.v) + hk * a.c.v_stride[1];
+
+  // LDS starts out as zeros: chunks behind the width stay so, which makes them count
+  // nothing, and keys that are not there are at worst old ones, whose scores are left out
+  for (int x = threadIdx.x * 16; x < 2 * KEYS * ROW; x += 1024 * kWaves)
+    *reinterpret_cast<u32x4*>(&kt[0][x]) = u32x4{};
+  for (int x = threadIdx.x * 16; x < 2 * S::VBYTES; x += 1024 * kWaves)
+    *reinterpret_cast<u32x4*>(&vt[0][x]) = u32x4{};
+  constexpr uint64_t every = KEYS == 64 ? ~(uint64_t)0 : (uint64_t(1) << KEYS) - 1;
 
   // a lane's key of a step: looked up and, later, written down for all waves
   auto look_up = [&](int block, int* slot) {
@@ -165,36 +202,115 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
     const uint64_t ok = __ballot(page >= 0);
     if (lane == 0) there[at] = ok;
   };
+  // 16-bit values on their way: unit x of a step is chunk x % (D / 8) of the 4 keys from
+  // 4 (x / (D / 8))
+  u32x4 vr[HALF ? VU : 1][4] = {};
   auto load = [&](int block) {
     const int at = (block - block0) & 3, buf = (block - block0) & 1;
+    const bool whole = (there[at] & every) == every;
+    const int row = threadIdx.x / CH, place = threadIdx.x % CH;   // and 256 / CH rows on
+    constexpr int NEXT = S::NEXT;
+    const int kc = place ^ (row & S::TURN);
+    int64_t ka[LOADS], va[LOADS];
 #pragma unroll
-    for (int u = 0; u < LOADS; ++u) {
-      const int first = (u * kWaves + wave) * 64;   // wave-uniform
-      const int row = (first + lane) / CH, place = (first + lane) % CH;
-      const int64_t ka = key_at[at][row], va = value_at[at][row];
-      const int kc = key_place(row, place), vc = value_place(row, place);
-      if (ka >= 0 && kc < chunks)
-        __builtin_amdgcn_global_load_lds((gptr_t)(kbase + ka + kc * VE),
-                                         (lptr_t)(&kt[buf][first * 16]), 16, 0, 0);
-      else
-        *reinterpret_cast<u32x4*>(&kt[buf][(first + lane) * 16]) = u32x4{};
-      if (va >= 0 && vc < chunks)
-        __builtin_amdgcn_global_load_lds((gptr_t)(vbase + va + vc * VE),
-                                         (lptr_t)(&vt[buf][first * 16]), 16, 0, 0);
-      else
-        *reinterpret_cast<u32x4*>(&vt[buf][(first + lane) * 16]) = u32x4{};
+    for (int u = 0; u < LOADS; ++u) ka[u] = key_at[at][row + u * NEXT];
+    if constexpr (HALF) {
+#pragma unroll
+      for (int u = 0; u < VU; ++u) {
+        const int x = u * 64 * kWaves + (int)threadIdx.x, ch = x % (D / VE), kg = x / (D / VE);
+        int64_t at4[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) at4[i] = value_at[at][(4 * kg + i) & (KEYS - 1)];
+        const bool in = ch < chunks && x < S::VUNITS;
+        if (whole) {
+          if (in) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              vr[u][i] = *reinterpret_cast<const u32x4*>(vbase + at4[i] + ch * VE);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            vr[u][i] = u32x4{};
+            if (in && at4[i] >= 0)
+              vr[u][i] = *reinterpret_cast<const u32x4*>(vbase + at4[i] + ch * VE);
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < LOADS; ++u) va[u] = value_at[at][row + u * NEXT];
+    }
+    if (whole) {
+      if (kc < chunks) {
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u)
+          __builtin_amdgcn_global_load_lds((gptr_t)(kbase + ka[u] + kc * VE),
+                                           (lptr_t)(&kt[buf][(u * kWaves + wave) * 1024]), 16, 0,
+                                           0);
+      }
+      if constexpr (!HALF) {
+        if (kc < chunks) {
+#pragma unroll
+          for (int u = 0; u < LOADS; ++u)
+            __builtin_amdgcn_global_load_lds((gptr_t)(vbase + va[u] + kc * VE),
+                                             (lptr_t)(&vt[buf][(u * kWaves + wave) * 1024]), 16,
+                                             0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < LOADS; ++u) {
+        const int first = (u * kWaves + wave) * 1024;   // wave-uniform
+        if (ka[u] >= 0 && kc < chunks)
+          __builtin_amdgcn_global_load_lds((gptr_t)(kbase + ka[u] + kc * VE),
+                                           (lptr_t)(&kt[buf][first]), 16, 0, 0);
+        if constexpr (!HALF) {
+          if (va[u] >= 0 && kc < chunks)
+            __builtin_amdgcn_global_load_lds((gptr_t)(vbase + va[u] + kc * VE),
+                                             (lptr_t)(&vt[buf][first]), 16, 0, 0);
+          else
+            *reinterpret_cast<u32x4*>(&vt[buf][first + lane * 16]) = u32x4{};
+        }
+      }
+    }
+  };
+  auto store_values = [&](int block) {
+    const int buf = (block - block0) & 1;
+#pragma unroll
+    for (int u = 0; u < VU; ++u) {
+      const int x = u * 64 * kWaves + (int)threadIdx.x, ch = x % (D / VE), kg = x / (D / VE);
+      if (x >= S::VUNITS) continue;
+      // keys 16 t + 8 y + 4 h .. + 3 stand behind each other for y = 0, 1
+      const int keys8 = 2 * (kg / 4) + kg % 2, y = kg / 2 % 2;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t pick = e & 1 ? 0x07060302u : 0x05040100u;
+        const u32x2 w{__builtin_amdgcn_perm(vr[u][1][e / 2], vr[u][0][e / 2], pick),
+                      __builtin_amdgcn_perm(vr[u][3][e / 2], vr[u][2][e / 2], pick)};
+        *reinterpret_cast<u32x2*>(&vt[buf][column_at(8 * ch + e, keys8) + 8 * y]) = w;
+      }
     }
   };
 
   f32x16 o[RB][DB];
   float top[RB], l[RB];
 
-  // WILD: of the values only those of `kind` count, and those that are not finite as 1,
-  // times whether a row sees the key.
-  auto sweep = [&](auto with_wild, Kind kind) {
-    constexpr bool WILD = decltype(with_wild)::value;
-    const bool counts = WILD && kind != Kind::finite;
-    __syncthreads();   // the last sweep has ended
+  // Lane offsets of the 8 chunks (key and value) of a step, whose other parts are constant:
+  // chunk 2x + h under the swizzle is 2x ^ (h ^ swizzle).
+  int ko[4], vo[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    ko[x] = c * ROW + 16 * ((2 * x + h) ^ (c & S::TURN));
+    vo[x] = column_at(c, 2 * x + h);
+  }
+
+  // One pass over the keys. Pass 0 is the only one unless values are not finite; the
+  // others count only the values of one kind (below).
+  auto sweep = [&](int pass) {
+    const Kind kind = (Kind)(pass - 1);
+    const bool counts = pass > 1;
+    __syncthreads();   // the last pass has ended
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       top[rb] = -INFINITY, l[rb] = 0.0f;
@@ -207,7 +323,10 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
       write_down(block0 + wave, page, slot);
     }
     __syncthreads();
-    if (block0 < block1) load(block0);
+    if (block0 < block1) {
+      load(block0);
+      if constexpr (HALF) store_values(block0);
+    }
     for (int block = block0; block < block1; ++block) {
       const int buf = (block - block0) & 1, j0 = block * KEYS;
       __builtin_amdgcn_s_waitcnt(0x0F70);   // this wave's loads have landed
@@ -216,22 +335,34 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
       int page = -1, slot = 0;
       if (mine) page = look_up(block + 2, &slot);
       if (block + 1 < block1) load(block + 1);
+      if (pass > 0) {   // in place, since only this step reads them
+        for (int x = (int)threadIdx.x * 4; x < S::VBYTES; x += 256 * kWaves) {
+          uint32_t* w = reinterpret_cast<uint32_t*>(&vt[buf][x]);
+          *w = only_kind<T>(*w, kind);
+        }
+        __syncthreads();
+      }
       if (j0 < some_see) {
         f32x16 s[RB][NB];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int rb = 0; rb < RB; ++rb) s[rb][b] = f32x16{};
+        read_ahead<KC * NB>(
+            [&](int n) {
+              const int b = n % NB, k = n / NB;
+              return *reinterpret_cast<const u32x4*>(
+                  &kt[buf][ko[k % 4] + 32 * b * ROW + 128 * (k / 4)]);
+            },
+            [&](int n, u32x4 kf) {
 #pragma unroll
-          for (int k = 0; k < KC; ++k) {
-            const u32x4 kf = *reinterpret_cast<const u32x4*>(
-                &kt[buf][(32 * b + c) * ROW + 16 * key_place(c, 2 * k + h)]);
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb) s[rb][b] = mul32<T>(kf, qf[rb][k], s[rb][b]);
-          }
-        }
+              for (int rb = 0; rb < RB; ++rb)
+                s[rb][n % NB] = mul32<T>(kf, qf[rb][n / NB], s[rb][n % NB]);
+            });
         const uint64_t ok = there[(block - block0) & 3];
-        constexpr uint64_t every = KEYS == 64 ? ~(uint64_t)0 : (uint64_t(1) << KEYS) - 1;
+        // whether this lane's row sees key k + 4 h of the step
+        const uint64_t ok_h = ok >> (4 * h);
+        auto sees = [&](int rb, int k) { return k < lim[rb] - j0 - 4 * h && (ok_h >> k & 1); };
         const bool masked = (ok & every) != every || j0 + KEYS > all_see;
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
@@ -239,16 +370,8 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const int k = 32 * b + result_row(i, h);
-                if (j0 + k >= lim[rb] || !(ok >> k & 1)) s[rb][b][i] = -INFINITY;
-                else s[rb][b][i] *= a.scale2;
-              }
-          } else {
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-              for (int i = 0; i < 16; ++i) s[rb][b][i] *= a.scale2;
+              for (int i = 0; i < 16; ++i)
+                if (!sees(rb, 32 * b + result_row(i, 0))) s[rb][b][i] = -INFINITY;
           }
           float high = s[rb][0][0];
 #pragma unroll
@@ -259,76 +382,62 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
           if (__any(high > top[rb])) {
             const float grown = fmaxf(top[rb], high);
             const float old =
-                __builtin_amdgcn_exp2f(top[rb] - (grown == -INFINITY ? 0.0f : grown));
+                __builtin_amdgcn_exp2f((top[rb] - (grown == -INFINITY ? 0.0f : grown)) * scale2);
             top[rb] = grown;
             l[rb] *= old;
 #pragma unroll
             for (int b = 0; b < DB; ++b)
               if (!counts) o[rb][b] *= old;
           }
-          const float base = top[rb] == -INFINITY ? 0.0f : top[rb];
+          const float base = top[rb] == -INFINITY ? 0.0f : -top[rb] * scale2;
           float sum = 0.0f;
 #pragma unroll
           for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              // (a row that sees the key has a finite score or makes NaN here)
-              s[rb][b][i] = __builtin_amdgcn_exp2f(s[rb][b][i] - base);
+              s[rb][b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][b][i], scale2, base));
               sum += s[rb][b][i];
             }
           l[rb] += sum;
+          if (counts) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                s[rb][b][i] = sees(rb, 32 * b + result_row(i, 0)) ? 1.0f : 0.0f;
+          }
         }
         if constexpr (HALF) {
           typedef T t8 __attribute__((ext_vector_type(8)));
-          const int i = lane & 15, part = lane >> 4 & 1;
+          u32x4 p[RB];
+          read_ahead<KEYS / 16 * DB>(
+              [&](int n) {
+                // (columns 32 apart differ in bit 2 of the swizzle)
+                const int step = n / DB, b = n % DB;
+                return *reinterpret_cast<const u32x4*>(
+                    &vt[buf][vo[step ^ (2 * (b & 1))] + 32 * 128 * b]);
+              },
+              [&](int n, u32x4 v) {
+                const int step = n / DB, b = n % DB;
 #pragma unroll
-          for (int step = 0; step < KEYS / 16; ++step) {
-            u32x4 p[RB];
+                for (int rb = 0; rb < RB; ++rb) {
+                  if (b == 0) {
+                    t8 x;
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-              t8 x;
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const int k = 32 * (step / 2) + result_row(8 * (step % 2) + e, h);
-                x[e] = (T)s[rb][step / 2][8 * (step % 2) + e];
-                if (counts) x[e] = (T)(j0 + k < lim[rb] && (ok >> k & 1) ? 1.0f : 0.0f);
-              }
-              p[rb] = __builtin_bit_cast(u32x4, x);
-            }
-#pragma unroll
-            for (int b = 0; b < DB; ++b) {
-              u32x4 v;
-#pragma unroll
-              for (int y = 0; y < 2; ++y) {
-                const int row = 16 * step + 8 * y + 4 * h + i / 4;
-                const int at = value_place(i / 4, 4 * b + 2 * part + i % 4 / 2);
-                const s16x4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (l16x4_t)(&vt[buf][row * ROW + 16 * at + 8 * (i % 2)]));
-                const u32x2 w2 = __builtin_bit_cast(u32x2, w);
-                v[2 * y] = w2[0], v[2 * y + 1] = w2[1];
-              }
-              if constexpr (WILD) {
-#pragma unroll
-                for (int u = 0; u < 4; ++u) v[u] = only_kind<T>(v[u], kind);
-              }
-#pragma unroll
-              for (int rb = 0; rb < RB; ++rb) o[rb][b] = mul32<T>(v, p[rb], o[rb][b]);
-            }
-          }
+                    for (int e = 0; e < 8; ++e) x[e] = (T)s[rb][step / 2][8 * (step % 2) + e];
+                    p[rb] = __builtin_bit_cast(u32x4, x);
+                  }
+                  o[rb][b] = mul32<T>(v, p[rb], o[rb][b]);
+                }
+              });
         } else {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int row = result_row(i, h);
-            if (counts) {
-#pragma unroll
-              for (int rb = 0; rb < RB; ++rb)
-                s[rb][0][i] = j0 + row < lim[rb] && (ok >> row & 1) ? 1.0f : 0.0f;
-            }
 #pragma unroll
             for (int b = 0; b < DB; ++b) {
-              uint32_t v = *reinterpret_cast<const uint32_t*>(
-                  &vt[buf][row * ROW + 16 * value_place(row, 8 * b + c / 4) + 4 * (c % 4)]);
-              if constexpr (WILD) v = only_kind<T>(v, kind);
+              const uint32_t v = *reinterpret_cast<const uint32_t*>(
+                  &vt[buf][row * ROW + 16 * ((8 * b + c / 4) ^ (row & S::TURN)) + 4 * (c % 4)]);
 #pragma unroll
               for (int rb = 0; rb < RB; ++rb)
                 o[rb][b] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(v), s[rb][0][i],
@@ -337,6 +446,8 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
           }
         }
       }
+      if constexpr (HALF)
+        if (block + 1 < block1) store_values(block + 1);
       if (mine) write_down(block + 2, page, slot);
     }
   };
@@ -380,9 +491,9 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
         }
       if (kind == Kind::finite && h == 0) {
         if (used > 1)
-          a.part_ml[split * rows + at] = float2{top[rb], sum};
+          a.part_ml[split * rows + at] = float2{top[rb] * scale2, sum};
         else if (a.lse)
-          a.lse[at] = sum == 0.0f ? INFINITY : top[rb] + __builtin_amdgcn_logf(sum);
+          a.lse[at] = sum == 0.0f ? INFINITY : top[rb] * scale2 + __builtin_amdgcn_logf(sum);
       }
     }
   };
@@ -390,22 +501,21 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
   // A value that is not finite makes its product with any probability so, zeros of rows
   // that do not see it among them. Then the keys are gone over again without such
   // values, and once more for each kind of them.
-  sweep(std::false_type{}, Kind::finite);
-  int wild = 0;
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-    for (int b = 0; b < DB; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) wild |= !__builtin_isfinite(o[rb][b][i]);
-  if (!__syncthreads_or(wild)) {
-    write(Kind::finite);
-  } else {
 #pragma unroll 1
-    for (int kind = 0; kind < 4; ++kind) {
-      sweep(std::true_type{}, (Kind)kind);
-      write((Kind)kind);
+  for (int pass = 0; pass < 5; ++pass) {
+    sweep(pass);
+    if (pass == 0) {
+      int wild = 0;
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) wild |= !__builtin_isfinite(o[rb][b][i]);
+      if (__syncthreads_or(wild)) continue;
     }
+    write(pass == 0 ? Kind::finite : (Kind)(pass - 1));
+    if (pass == 0) break;
   }
 }
 
@@ -463,6 +573,7 @@ __global__ void __launch_bounds__(64 * kWaves) k_weights_chunk(AttentionArgs a) 
     for (int i = 0; i < KC; ++i)
       qf[i] = 2 * i + h < chunks ? load_loose(q + (2 * i + h) * VE) : u32x4{};
     const bool masked = j0 + 64 > seen_keys(a, t, row) || row + 32 > rows;
+    const int left = lim - j0 - 4 * h;   // keys of this lane that its row sees
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       f32x16 z{};
@@ -471,7 +582,7 @@ __global__ void __launch_bounds__(64 * kWaves) k_weights_chunk(AttentionArgs a) 
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const float p = __builtin_amdgcn_exp2f(z[i] * a.scale2 - lse);
-        sum[b][i] += masked && j0 + 32 * b + result_row(i, h) >= lim ? 0.0f : p;
+        sum[b][i] += masked && 32 * b + result_row(i, 0) >= left ? 0.0f : p;
       }
     }
   }

@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
         for (int b = 0; b < KB; ++b)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (j0 + 16 * b + 4 * g + i >= lim || !(there >> (4 * b + i) & 1)) s[b][i] = -INFINITY;
+            if (16 * b + i >= lim - j0 - 4 * g || !(there >> (4 * b + i) & 1)) s[b][i] = -INFINITY;
       }
       if (a.plan.pitch && m < t.rows) {
 #pragma unroll
