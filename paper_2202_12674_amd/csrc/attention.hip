@@ -53,7 +53,7 @@ size_t carve(AttentionArgs& a, void* workspace) {
   return std::max<size_t>(c.off, 256);
 }
 
-// Joins the splits of one tile: out = sum_i 2^(m_i - m) part_i / sum_i 2^(m_i - m) l_i.
+// Joins the splits of 16 rows of a tile: out = sum_i 2^(m_i - m) part_i / sum_i 2^(m_i - m) l_i.
 // Four values of a row per thread.
 template <typename T>
 __global__ void __launch_bounds__(256) k_attention_join(AttentionArgs a, int block, int least) {
@@ -62,10 +62,10 @@ __global__ void __launch_bounds__(256) k_attention_join(AttentionArgs a, int blo
   const int per = split_blocks(t.keys, block, a.plan.splits, least);
   const int used = ((t.keys + block - 1) / block + per - 1) / per;
   if (used <= 1) return;
-  const int hk = blockIdx.y, dim = (int)a.c.dim, quads = dim / 4;
+  const int hk = blockIdx.y, dim = (int)a.c.dim, quads = dim / 4, y0 = 16 * blockIdx.z;
   const int64_t rows = a.tokens * a.heads;
-  for (int x = threadIdx.x; x < t.rows * quads; x += 256) {
-    const int y = x / quads, d = x % quads * 4;
+  for (int x = threadIdx.x; x < min(16, t.rows - y0) * quads; x += 256) {
+    const int y = y0 + x / quads, d = x % quads * 4;
     const int tok = (t.row0 + y) / a.group, h = hk * a.group + (t.row0 + y) % a.group;
     const int64_t at = (t.first + tok) * a.heads + h;
     float m = -INFINITY;
@@ -91,27 +91,39 @@ __global__ void __launch_bounds__(256) k_attention_join(AttentionArgs a, int blo
 }
 
 // weight_out = weight + the probabilities of few rows, from their stored scores. A
-// thread per key: rows are summed in order.
-__global__ void __launch_bounds__(256) k_weights_few(AttentionArgs a) {
+// thread has four keys: their rows are summed in order.
+constexpr int kWeightKeys = 1024;   // per block
+__global__ void __launch_bounds__(kWeightKeys / 4) k_weights_few(AttentionArgs a) {
   const int s = blockIdx.z, hk = blockIdx.y;
   const int L = cache_length(a.c, s);
-  const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int j = blockIdx.x * kWeightKeys + 4 * (int)threadIdx.x;
   if (j >= L) return;
-  int slot;
-  const int page = cache_page(a.c, s, (int)j, &slot);
-  if (page < 0) return;
   int64_t first;
   int n;
   sequence_rows(a, s, &first, &n);
-  float gain = 0.0f;
+  float gain[4] = {};
   for (int i = 0; i < n; ++i) {
-    if (a.causal && j > (int64_t)L - n + i) continue;
+    const int seen = a.causal ? L - n + i + 1 - j : L - j;   // of these keys and on
+    if (seen <= 0) continue;
     const int64_t row = (first + i) * a.heads + hk * a.group;
-    for (int h = 0; h < a.group; ++h)
-      gain += __builtin_amdgcn_exp2f(a.scores[(row + h) * a.plan.pitch + j] - a.lse[row + h]);
+#pragma unroll 4
+    for (int h = 0; h < a.group; ++h) {
+      const float lse = a.lse[row + h];
+      const f32x4 z = *reinterpret_cast<const f32x4*>(a.scores + (row + h) * a.plan.pitch + j);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        gain[k] += k < seen ? __builtin_amdgcn_exp2f(z[k] - lse) : 0.0f;
+    }
   }
-  const float old = a.c.weight[page * a.c.weight_stride[0] + hk * a.c.weight_stride[1] + slot];
-  a.weight_out[page * a.ws.outer + hk * a.ws.head + slot] = old + gain;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (j + k >= L) break;
+    int slot;
+    const int page = cache_page(a.c, s, j + k, &slot);
+    if (page < 0) continue;
+    const float old = a.c.weight[page * a.c.weight_stride[0] + hk * a.c.weight_stride[1] + slot];
+    a.weight_out[page * a.ws.outer + hk * a.ws.head + slot] = old + gain[k];
+  }
 }
 
 }  // namespace
@@ -128,7 +140,7 @@ size_t attention_workspace(const lssvm_cache& c, int64_t tokens, int heads, bool
 
 template <typename T>
 hipError_t join(const AttentionArgs& a, hipStream_t stream) {
-  const dim3 grid((unsigned)a.plan.tiles, (unsigned)a.c.heads);
+  const dim3 grid((unsigned)a.plan.tiles, (unsigned)a.c.heads, (unsigned)a.plan.rows / 16);
   const int block = a.plan.few ? few_keys<T> : chunk_keys<T>;
   k_attention_join<T><<<grid, 256, 0, stream>>>(a, block, a.plan.few ? kFewLeast : kChunkLeast);
   return hipGetLastError();
@@ -147,9 +159,9 @@ hipError_t launch_attention(AttentionArgs a, void* workspace, hipStream_t stream
   }
   if (e != hipSuccess || !a.accumulate) return e;
   if (!a.plan.few) return launch_weights_chunk(a, stream);
-  k_weights_few<<<dim3((unsigned)((a.c.columns * a.c.page + 255) / 256), (unsigned)a.c.heads,
-                       (unsigned)a.c.sequences),
-                  256, 0, stream>>>(a);
+  k_weights_few<<<dim3((unsigned)((a.c.columns * a.c.page + kWeightKeys - 1) / kWeightKeys),
+                       (unsigned)a.c.heads, (unsigned)a.c.sequences),
+                  kWeightKeys / 4, 0, stream>>>(a);
   return hipGetLastError();
 }
 

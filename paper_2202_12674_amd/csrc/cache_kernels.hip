@@ -13,14 +13,19 @@ constexpr int kThreads = 256;
 // ------------------------------------------------------ rotary positions ----
 
 // cos and sin of `angle`, to about an ulp of fp32: the quarter turns are taken off in
-// fp64 (pi/2 in two parts), so that positions of millions lose nothing.
+// fp64 (pi/2 in two parts), so that positions of millions lose nothing; what is left is
+// at most pi/4, where the Taylor polynomials of degree 9 and 10 are off by 2e-9 and 2e-10.
 LSSVM_DEV void turn(double angle, float* c, float* s) {
   const double k = rint(angle * 0.63661977236758134308);
-  double r = fma(-k, 1.57079632679489655800, angle);
-  r = fma(-k, 6.12323399573676603587e-17, r);
-  float sr, cr;
-  sincosf((float)r, &sr, &cr);
-  const int quarter = (int)((int64_t)k & 3);
+  double rest = fma(-k, 1.57079632679489655800, angle);
+  rest = fma(-k, 6.12323399573676603587e-17, rest);
+  const float r = (float)rest, q = r * r;
+  const float sr = r + r * q * (-1.0f / 6 + q * (1.0f / 120 + q * (-1.0f / 5040 + q * (1.0f / 362880))));
+  const float cr = 1.0f + q * (-0.5f + q * (1.0f / 24 + q * (-1.0f / 720 + q * (1.0f / 40320 +
+                                                                             q * (-1.0f / 3628800)))));
+  // of k, the last two bits (k is a whole number below 2^53 in size, or nothing is left
+  // to tell them by)
+  const int quarter = (int)(k - 4.0 * floor(0.25 * k));
   const float a = quarter & 1 ? sr : cr, b = quarter & 1 ? cr : sr;
   *c = quarter == 1 || quarter == 2 ? -a : a;
   *s = quarter >= 2 ? -b : b;
@@ -38,82 +43,85 @@ __host__ __device__ inline int copy_chunks(int values) {
   return (values + kVec<T> - 1) / kVec<T>;
 }
 
-// The factors of the pairs of chunk `at`.
+// The factors of the pairs of chunk `at` (of its last pair behind the last one).
 template <typename T, bool INTER>
 struct Factors {
   static constexpr int N = INTER ? kVec<T> / 2 : kVec<T>;
   float c[N], s[N];
   LSSVM_DEV void set(const RotaryArgs& a, int64_t t, int at) {
+    double f[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = a.freqs[min(at * N + i, a.pairs - 1)];
     const double p = a.wide_positions
                          ? (double)static_cast<const int64_t*>(a.positions)[t]
                          : (double)static_cast<const int32_t*>(a.positions)[t];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int pair = at * N + i;
-      if (pair >= a.pairs) break;
-      turn(p * a.freqs[pair], &c[i], &s[i]);
+      turn(p * f[i], &c[i], &s[i]);
       c[i] *= a.scale;
       s[i] *= a.transpose ? -a.scale : a.scale;
     }
   }
 };
 
-// Turns the pairs of chunk `at` of one head. All of the chunk is read before any of
-// it is written, so y may be x.
+// Chunk `at` of the pairs of one head: read, turned, written. All of it is read before
+// any is written, so y may be x.
 template <typename T, bool INTER>
-LSSVM_DEV void turn_chunk(const Factors<T, INTER>& f, const T* x, T* y, int at, int pairs) {
-  constexpr int N = Factors<T, INTER>::N, W = kVec<T>;
-  const int left = pairs - at * N;
-  if constexpr (INTER) {
-    x += at * W;
-    y += at * W;
-    Loose<T, W> v;
+struct Pairs {
+  static constexpr int N = Factors<T, INTER>::N, W = kVec<T>;
+  typedef T vec __attribute__((ext_vector_type(W)));
+  vec a, b;   // interleaved: a alone
+  static LSSVM_DEV vec get(const T* x) {
+    return __builtin_bit_cast(vec, *reinterpret_cast<const Loose<T, W>*>(x));
+  }
+  static LSSVM_DEV void put(T* y, vec v) {
+    *reinterpret_cast<Loose<T, W>*>(y) = __builtin_bit_cast(Loose<T, W>, v);
+  }
+  LSSVM_DEV void read(const T* x, int at, int pairs) {
+    const int left = pairs - at * N;
+    x += at * (INTER ? W : N);
     if (left >= N) {
-      v = *reinterpret_cast<const Loose<T, W>*>(x);
+      a = get(x);
+      if constexpr (!INTER) b = get(x + pairs);
     } else {
-      for (int i = 0; i < 2 * left; ++i) v.v[i] = x[i];
-    }
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float p = (float)v.v[2 * i], q = (float)v.v[2 * i + 1];
-      v.v[2 * i] = (T)(p * f.c[i] - q * f.s[i]);
-      v.v[2 * i + 1] = (T)(q * f.c[i] + p * f.s[i]);
-    }
-    if (left >= N) {
-      *reinterpret_cast<Loose<T, W>*>(y) = v;
-    } else {
-      for (int i = 0; i < 2 * left; ++i) y[i] = v.v[i];
-    }
-  } else {
-    x += at * N;
-    y += at * N;
-    Loose<T, W> a, b;
-    if (left >= N) {
-      a = *reinterpret_cast<const Loose<T, W>*>(x);
-      b = *reinterpret_cast<const Loose<T, W>*>(x + pairs);
-    } else {
-      for (int i = 0; i < left; ++i) {
-        a.v[i] = x[i];
-        b.v[i] = x[i + pairs];
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float p = (float)a.v[i], q = (float)b.v[i];
-      a.v[i] = (T)(p * f.c[i] - q * f.s[i]);
-      b.v[i] = (T)(q * f.c[i] + p * f.s[i]);
-    }
-    if (left >= N) {
-      *reinterpret_cast<Loose<T, W>*>(y) = a;
-      *reinterpret_cast<Loose<T, W>*>(y + pairs) = b;
-    } else {
-      for (int i = 0; i < left; ++i) {
-        y[i] = a.v[i];
-        y[i + pairs] = b.v[i];
+      for (int i = 0; i < W; ++i) {
+        const bool in = (INTER ? i / 2 : i) < left;
+        a[i] = in ? x[i] : (T)0.0f;
+        if constexpr (!INTER) b[i] = in ? x[i + pairs] : (T)0.0f;
       }
     }
   }
-}
+  LSSVM_DEV void turn(const Factors<T, INTER>& f) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if constexpr (INTER) {
+        const float p = (float)a[2 * i], q = (float)a[2 * i + 1];
+        a[2 * i] = (T)(p * f.c[i] - q * f.s[i]);
+        a[2 * i + 1] = (T)(q * f.c[i] + p * f.s[i]);
+      } else {
+        const float p = (float)a[i], q = (float)b[i];
+        a[i] = (T)(p * f.c[i] - q * f.s[i]);
+        b[i] = (T)(q * f.c[i] + p * f.s[i]);
+      }
+    }
+  }
+  LSSVM_DEV void write(T* y, int at, int pairs) const {
+    const int left = pairs - at * N;
+    y += at * (INTER ? W : N);
+    if (left >= N) {
+      put(y, a);
+      if constexpr (!INTER) put(y + pairs, b);
+    } else {
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        if ((INTER ? i / 2 : i) >= left) break;
+        y[i] = a[i];
+        if constexpr (!INTER) y[i + pairs] = b[i];
+      }
+    }
+  }
+};
 
 // Copies chunk `at` of `n` values.
 template <typename T>
@@ -154,15 +162,22 @@ __global__ void __launch_bounds__(kThreads) k_rotary(RotaryArgs a, int chunks, i
   if (t >= a.tokens) return;
   const T* x = static_cast<const T*>(a.x) + t * a.xs.outer;
   T* y = static_cast<T*>(a.out) + t * a.os.outer;
+  if (at >= turned) {
+    for (int h = group; h < a.heads; h += groups)
+      copy_chunk(x + h * a.xs.head + 2 * a.pairs, y + h * a.os.head + 2 * a.pairs, at - turned,
+                 a.dim - 2 * a.pairs);
+    return;
+  }
+  // the next head is read before this one is written
+  Pairs<T, INTER> now, next;
+  now.read(x + group * a.xs.head, at, a.pairs);
   Factors<T, INTER> f;
-  if (at < turned) f.set(a, t, at);
+  f.set(a, t, at);
   for (int h = group; h < a.heads; h += groups) {
-    const T* xh = x + h * a.xs.head;
-    T* yh = y + h * a.os.head;
-    if (at < turned)
-      turn_chunk<T, INTER>(f, xh, yh, at, a.pairs);
-    else
-      copy_chunk(xh + 2 * a.pairs, yh + 2 * a.pairs, at - turned, a.dim - 2 * a.pairs);
+    if (h + groups < a.heads) next.read(x + (h + groups) * a.xs.head, at, a.pairs);
+    now.turn(f);
+    now.write(y + h * a.os.head, at, a.pairs);
+    now = next;
   }
 }
 
@@ -179,12 +194,32 @@ hipError_t by_dtype(int dtype, F f) {
 template <typename T, bool INTER>
 __global__ void __launch_bounds__(kThreads) k_append(AppendArgs a, int chunks, int turned,
                                                      int copied, int groups) {
+  // every `stride`-th offset, so that the search for a token's sequence is one in LDS
+  __shared__ int32_t some[kThreads];
+  const int sequences = (int)a.c.sequences, stride = (sequences + kThreads - 1) / kThreads;
+  const int held = (sequences + stride - 1) / stride;
+  if ((int)threadIdx.x < held) some[threadIdx.x] = a.offsets[threadIdx.x * stride];
+  __syncthreads();
   int at, group;
   const int64_t t = split(split((int64_t)blockIdx.x * kThreads + threadIdx.x, chunks, &at),
                           groups, &group);
   if (t >= a.k.tokens) return;
+  const T* xk = static_cast<const T*>(a.k.x) + t * a.k.xs.outer;
+  const T* xv = static_cast<const T*>(a.v) + t * a.vs.outer;
+  Factors<T, INTER> f;
+  Pairs<T, INTER> pairs;
+  if (at < turned) {
+    pairs.read(xk + group * a.k.xs.head, at, a.k.pairs);
+    f.set(a.k, t, at);
+  }
   // the sequence: the last whose first token is not behind t
-  int lo = 0, hi = (int)a.c.sequences;
+  int lo = 0, hi = held;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (some[mid] <= t) lo = mid; else hi = mid;
+  }
+  lo *= stride;
+  hi = min(lo + stride, sequences);
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (a.offsets[mid] <= t) lo = mid; else hi = mid;
@@ -198,13 +233,11 @@ __global__ void __launch_bounds__(kThreads) k_append(AppendArgs a, int chunks, i
   if (page < 0) return;
   T* k = static_cast<T*>(a.c.k) + page * a.c.k_stride[0] + slot * a.c.k_stride[2];
   T* v = static_cast<T*>(a.c.v) + page * a.c.v_stride[0] + slot * a.c.v_stride[2];
-  const T* xk = static_cast<const T*>(a.k.x) + t * a.k.xs.outer;
-  const T* xv = static_cast<const T*>(a.v) + t * a.vs.outer;
-  Factors<T, INTER> f;
-  if (at < turned) f.set(a.k, t, at);
   for (int h = group; h < a.k.heads; h += groups) {
     if (at < turned) {
-      turn_chunk<T, INTER>(f, xk + h * a.k.xs.head, k + h * a.c.k_stride[1], at, a.k.pairs);
+      if (h != group) pairs.read(xk + h * a.k.xs.head, at, a.k.pairs);
+      pairs.turn(f);
+      pairs.write(k + h * a.c.k_stride[1], at, a.k.pairs);
     } else if (at < turned + copied) {
       copy_chunk(xk + h * a.k.xs.head + 2 * a.k.pairs, k + h * a.c.k_stride[1] + 2 * a.k.pairs,
                  at - turned, a.k.dim - 2 * a.k.pairs);
