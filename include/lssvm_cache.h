@@ -41,7 +41,7 @@ enum { LSSVM_BF16 = 2, LSSVM_F16 = 3 };
  * dim contiguous values, with strides in elements; v and weight alike (a weight is
  * one float per key, its slots contiguous). Strides are free as long as no two rows
  * overlap and rows of k and v begin on 16 bytes, so heads may stand before or behind
- * the slots of a page; slots are at most 2^26 values apart. */
+ * the slots of a page; slots are at most 2^24 values apart. */
 typedef struct lssvm_cache {
     void* k;
     void* v;

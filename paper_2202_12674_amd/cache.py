@@ -8,8 +8,9 @@ back. The calls can be captured into a HIP graph.
 from __future__ import annotations
 
 import ctypes
+import functools
 
-from ._binding import _check, _torch, _workspace, alloc_workspace, lib
+from ._binding import OK, _check, _workspace, alloc_workspace, lib
 
 F32, BF16, F16 = 1, 2, 3
 SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
@@ -41,32 +42,45 @@ _SIGS = {
                                _P, ctypes.c_size_t, _P]),
     "lssvm_cache_evict": (_I32, [_C, _C, _I64, _I64, _P, _P]),
 }
-_loaded = None
 
 
+@functools.cache
+def _torch():
+    import torch
+    return torch
+
+
+@functools.cache
 def _lib():
-    global _loaded
-    if _loaded is None:
-        L = lib()
-        for name, (res, args) in _SIGS.items():
-            fn = getattr(L, name)
-            fn.restype, fn.argtypes = res, args
-        _loaded = L
-    return _loaded
+    L = lib()
+    for name, (res, args) in _SIGS.items():
+        fn = getattr(L, name)
+        fn.restype, fn.argtypes = res, args
+    return L
+
+
+@functools.cache
+def _codes():
+    torch = _torch()
+    return {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
 
 def _code(dtype) -> int:
-    torch = _torch()
-    codes = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
-    if dtype not in codes:
+    code = _codes().get(dtype)
+    if code is None:
         raise TypeError(f"unsupported dtype {dtype}; use float32, bfloat16 or float16")
-    return codes[dtype]
+    return code
+
+
+@functools.lru_cache(maxsize=256)
+def _two(outer: int, head: int, *_):
+    """The first two strides of a tensor, for the library to read."""
+    return _Two(outer, head)
 
 
 def _gpu(t, name: str, dims: int, dtype=None, device=None):
     """t, a GPU tensor of `dims` dimensions with contiguous last one, else an error."""
-    torch = _torch()
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    if not isinstance(t, _torch().Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
     if t.dim() != dims:
         raise ValueError(f"{name} must have {dims} dimensions, not {tuple(t.shape)}")
@@ -74,22 +88,30 @@ def _gpu(t, name: str, dims: int, dtype=None, device=None):
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
     if device is not None and t.device != device:
         raise ValueError(f"{name} must be on {device}, not {t.device}")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
     return t
 
 
-def _call(device, name: str, *args) -> None:
-    """The library's call on the device's current stream, with that device current."""
+@functools.cache
+def _raw_stream():
+    """The handle of a device's current stream; where torch offers it, without a Stream
+    object around it, which costs half as much as a launch."""
     torch = _torch()
-    fn = getattr(_lib(), name)
-    stream = torch.cuda.current_stream(device).cuda_stream
-    if torch.cuda.current_device() == device.index:
-        code = fn(*args, stream)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _call(device, fn, *args) -> None:
+    """The library's call on the device's current stream, with that device current."""
+    cuda, index = _torch().cuda, device.index
+    if cuda.current_device() == index:
+        code = fn(*args, _raw_stream()(index))
     else:
-        with torch.cuda.device(device):
-            code = fn(*args, stream)
-    _check(code)
+        with cuda.device(device):
+            code = fn(*args, _raw_stream()(index))
+    if code != OK:
+        _check(code)
 
 
 class PagedCache:
@@ -200,14 +222,14 @@ def rotary(x, positions, freqs, scale: float = 1.0, interleaved: bool = False,
     _gpu(x, "x", 3)
     code = _code(x.dtype)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = torch.empty_like(x)
     else:
         _gpu(out, "out", 3, x.dtype, x.device)
         if out.shape != x.shape:
             raise ValueError(f"out must have the shape of x, {tuple(x.shape)}")
     tokens, heads, dim = x.shape
-    _call(x.device, "lssvm_rotary", x.data_ptr(), _Two(*x.stride()[:2]), out.data_ptr(),
-          _Two(*out.stride()[:2]), tokens, heads, dim,
+    _call(x.device, _lib().lssvm_rotary, x.data_ptr(), _two(*x.stride()), out.data_ptr(),
+          _two(*out.stride()), tokens, heads, dim,
           *_angles(positions, freqs, tokens, x.device), scale, interleaved, transpose, code)
     return out
 
@@ -229,8 +251,8 @@ def cache_append(cache, k, v, offsets, positions=None, freqs=None, scale: float 
         raise ValueError("positions and freqs are given together")
     angles = (None, 0, None, 0) if freqs is None else _angles(positions, freqs, tokens,
                                                               cache.device)
-    _call(cache.device, "lssvm_cache_append", cache._ref, k.data_ptr(), _Two(*k.stride()[:2]),
-          v.data_ptr(), _Two(*v.stride()[:2]), tokens, _offsets(offsets, cache), *angles, scale,
+    _call(cache.device, _lib().lssvm_cache_append, cache._ref, k.data_ptr(), _two(*k.stride()),
+          v.data_ptr(), _two(*v.stride()), tokens, _offsets(offsets, cache), *angles, scale,
           interleaved)
 
 
@@ -254,7 +276,7 @@ def attention(q, cache, offsets, scale: float | None = None, causal: bool = True
     _rows(q, "q", cache)
     tokens, heads, dim = q.shape
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q)
     else:
         _rows(out, "out", cache, heads)
         if out.shape[0] != tokens:
@@ -274,10 +296,10 @@ def attention(q, cache, offsets, scale: float | None = None, causal: bool = True
         _workspace(workspace, cache.device)
         if not workspace.is_contiguous():
             raise ValueError("workspace must be contiguous")
-    _call(cache.device, "lssvm_attention", cache._ref, q.data_ptr(), _Two(*q.stride()[:2]),
+    _call(cache.device, _lib().lssvm_attention, cache._ref, q.data_ptr(), _two(*q.stride()),
           tokens, heads, _offsets(offsets, cache), dim ** -0.5 if scale is None else scale, causal,
-          accumulate, weight_out.data_ptr() if w else None, _Two(*w) if w else None,
-          out.data_ptr(), _Two(*out.stride()[:2]), workspace.data_ptr(),
+          accumulate, weight_out.data_ptr() if w else None, _two(*w) if w else None,
+          out.data_ptr(), _two(*out.stride()), workspace.data_ptr(),
           workspace.numel() * workspace.element_size())
     return out
 
@@ -299,6 +321,6 @@ def cache_evict(cache, target, budget: int, recent: int = 0, kept=None):
         _gpu(kept, "kept", 3, torch.int32, cache.device)
         if tuple(kept.shape) != shape or not kept.is_contiguous():
             raise ValueError(f"kept must be {shape} and contiguous")
-    _call(cache.device, "lssvm_cache_evict", cache._ref, target._ref, budget, recent,
+    _call(cache.device, _lib().lssvm_cache_evict, cache._ref, target._ref, budget, recent,
           kept.data_ptr() if kept is not None else None)
     return kept

@@ -14,6 +14,7 @@ namespace lssvm {
 // `splits` workgroups, whose parts one more launch joins.
 struct AttentionPlan {
   bool few;          // tiles of 16 rows, keys streamed through registers
+  bool wide;         // ... by eight waves in place of four
   int rows;          // rows per tile
   int64_t tiles;     // at most so many tiles of one head
   int splits;
@@ -76,8 +77,11 @@ LSSVM_DEV bool find_tile(const AttentionArgs& a, int64_t index, int rows, Tile* 
   int64_t before = 0;
   for (int base = 0; base < a.c.sequences; base += 64) {
     int64_t first = 0;
-    int n = 0;
-    if (base + lane < a.c.sequences) sequence_rows(a, base + lane, &first, &n);
+    int n = 0, length = 0;
+    if (base + lane < a.c.sequences) {
+      sequence_rows(a, base + lane, &first, &n);
+      length = cache_length(a.c, base + lane);
+    }
     const int64_t mine = ((int64_t)n * a.group + rows - 1) / rows;
     int64_t to = mine;
     for (int d = 1; d < 64; d <<= 1) {
@@ -91,7 +95,7 @@ LSSVM_DEV bool find_tile(const AttentionArgs& a, int64_t index, int rows, Tile* 
       t->s = __builtin_amdgcn_readfirstlane(base + at);
       t->first = __shfl(first, at);
       t->n = __builtin_amdgcn_readfirstlane(__shfl(n, at));
-      t->length = __builtin_amdgcn_readfirstlane(cache_length(a.c, t->s));
+      t->length = __builtin_amdgcn_readfirstlane(__shfl(length, at));
       t->row0 = __builtin_amdgcn_readfirstlane((int)(index - skipped) * rows);
       t->rows = min(rows, t->n * a.group - t->row0);
       t->keys = seen_keys(a, *t, t->row0 + t->rows - 1);

@@ -11,6 +11,9 @@ hipError_t launch_weights_chunk(const AttentionArgs& a, hipStream_t stream);
 namespace {
 
 constexpr int64_t kCUs = 256;
+#ifndef WIDE_MAX
+#define WIDE_MAX 768
+#endif
 constexpr int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 
 AttentionPlan make_plan(const lssvm_cache& c, int64_t tokens, int heads, bool accumulate) {
@@ -27,6 +30,10 @@ AttentionPlan make_plan(const lssvm_cache& c, int64_t tokens, int heads, bool ac
   const int64_t want = std::max<int64_t>(1, (p.few ? 8 : 2) * kCUs / whole);
   p.splits = (int)std::max<int64_t>(
       1, std::min<int64_t>({want, (most + 127) / 128, p.few ? 64 : 16}));
+  if (p.few && whole <= kCUs && most <= WIDE_MAX) {
+    p.wide = true;
+    p.splits = 1;
+  }
   p.pitch = accumulate && p.few ? round_up(most, 32) : 0;
   return p;
 }

@@ -2,10 +2,15 @@
 // cache: include/lssvm_cache.h.
 #include "attention.h"
 
+#include <climits>
+
 namespace lssvm {
 namespace {
 
-constexpr int kWaves = 4;
+// Third word of a raw buffer resource (32-bit data, no swizzle, no stride).
+constexpr int kBufferWord3 = 0x00020000;
+typedef const __attribute__((address_space(4))) int32_t* const_i32;
+__device__ const u32x4 kNothing[1] = {};
 
 // The matrix cores on 16 keys x 16 rows.
 template <typename T>
@@ -64,7 +69,7 @@ struct Shape {
 // Keys of the next step are loaded as soon as the scores are formed, values as soon
 // as the product is issued, so that a wave has loads in flight all the time. BLOCKS:
 // the pages hold whole runs of 16 keys, whose page is then looked up once.
-template <typename T, int D, bool BLOCKS>
+template <typename T, int D, bool BLOCKS, int kWaves>
 __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) {
   using S = Shape<T, D>;
   constexpr int VE = S::VE, KB = S::KB, KEYS = S::KEYS, KC = S::KC, CE = S::CE, CW = S::CW,
@@ -107,78 +112,108 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
   const T* vbase = static_cast<const T*>(a.c.v) + hk * a.c.v_stride[1];
   const int ks = (int)a.c.k_stride[2], vs = (int)a.c.v_stride[2];
 
-  // where the keys of a step are: page (or -1) and slot; of every 16 keys, or of
-  // this lane's key
+  // Where a step's keys are: page and slot of every 16 of them (or of this lane's one)
+  // and how many keys of the split follow from there. The pages' numbers are checked
+  // when they have arrived.
+  constexpr int RUNS = BLOCKS ? KB : 1;
   struct Place {
-    int page[BLOCKS ? KB : 1], slot[BLOCKS ? KB : 1];
+    int page[RUNS], slot[RUNS], left[RUNS];
   };
-  auto locate = [&](int block) {
+  const int size = (int)a.c.page, end = min(t.length, block1 * KEYS);
+  int column[RUNS], slot[RUNS], key[RUNS];   // of the next step to be located
+  const int columns_on = kWaves * KEYS / size, slots_on = kWaves * KEYS - columns_on * size;
+  auto locate = [&]() {
     Place p;
-    if constexpr (BLOCKS) {
 #pragma unroll
-      for (int b = 0; b < KB; ++b) {
-        const int j = block * KEYS + 16 * b;
-        p.page[b] = -1, p.slot[b] = 0;
-        if (j < t.length) {
-          p.page[b] = cache_page(a.c, t.s, j, &p.slot[b]);
-        }
-      }
-    } else {
-      const int j = block * KEYS + (lane & (KEYS - 1));
-      p.page[0] = -1, p.slot[0] = 0;
-      if (j < t.length) p.page[0] = cache_page(a.c, t.s, j, &p.slot[0]);
+    for (int b = 0; b < RUNS; ++b) {
+      const int64_t at = t.s * a.c.table_stride + min(column[b], (int)a.c.columns - 1);
+      if constexpr (BLOCKS)
+        p.page[b] = reinterpret_cast<const_i32>(reinterpret_cast<uintptr_t>(a.c.table))[at];
+      else
+        p.page[b] = a.c.table[at];
+      p.slot[b] = slot[b];
+      p.left[b] = end - key[b];
+      key[b] += kWaves * KEYS;
+      column[b] += columns_on;
+      slot[b] += slots_on;
+      if (slot[b] >= size) slot[b] -= size, ++column[b];
     }
     return p;
   };
+  // Rows of a run through a buffer as long as they are: what lies behind it, and chunks
+  // behind the width, are read as zeros. Other keys are read one by one, zeros for them
+  // from a place of their own; no load hangs on a branch.
+  const int bytes = (int)sizeof(T);
+  int ko[BLOCKS ? KC : 1], vo[BLOCKS ? 4 : 1][NC];
+  if constexpr (BLOCKS) {
+#pragma unroll
+    for (int c = 0; c < KC; ++c)
+      ko[c] = (4 * c + g) * VE < dim ? (m * ks + (4 * c + g) * VE) * bytes : INT_MIN;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int part = 0; part < NC; ++part) {
+        const int d = 16 * CE * part + CE * m;
+        vo[i][part] = d < dim ? ((4 * g + i) * vs + d) * bytes : INT_MIN;
+      }
+  }
+  auto run = [&](const T* base, int64_t page_stride, int stride, const Place& p, int b) {
+    const bool ok = p.page[b] >= 0 && p.page[b] < a.c.pages && p.left[b] > 0;
+    const T* at = base + (int64_t)(ok ? p.page[b] : 0) * page_stride + (int64_t)p.slot[b] * stride;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(at), (short)0,
+                                             ok ? min(p.left[b], 16) * stride * bytes : 0,
+                                             kBufferWord3);
+  };
+  auto one = [&](const T* base, int64_t page_stride, int stride, const Place& p, int from) {
+    const int page = __shfl(p.left[0] > 0 ? p.page[0] : -1, from), at = __shfl(p.slot[0], from);
+    return page >= 0 && page < a.c.pages ? base + page * page_stride + (int64_t)at * stride
+                                         : nullptr;
+  };
+  const T* nothing = reinterpret_cast<const T*>(kNothing);
   u32x4 kf[KB][KC];
   auto load_keys = [&](const Place& p) {
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
-      const T* k;
       if constexpr (BLOCKS) {
-        k = kbase + (int64_t)max(p.page[b], 0) * a.c.k_stride[0] + (int64_t)p.slot[b] * ks;
-        k += m * ks + g * VE;
-      } else {
-        const int page = __shfl(p.page[0], 16 * b + m), slot = __shfl(p.slot[0], 16 * b + m);
-        k = kbase + (int64_t)max(page, 0) * a.c.k_stride[0] + (int64_t)slot * ks + g * VE;
-      }
+        const auto r = run(kbase, a.c.k_stride[0], ks, p, b);
 #pragma unroll
-      for (int c = 0; c < KC; ++c) {
-        kf[b][c] = u32x4{};
-        if ((4 * c + 3) * VE < dim || (4 * c + g) * VE < dim)
-          kf[b][c] = *reinterpret_cast<const u32x4*>(k + 4 * c * VE);
+        for (int c = 0; c < KC; ++c)
+          kf[b][c] = __builtin_amdgcn_raw_buffer_load_b128(r, ko[c], 0, 0);
+      } else {
+        const T* k = one(kbase, a.c.k_stride[0], ks, p, 16 * b + m);
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          const int at = (4 * c + g) * VE;
+          kf[b][c] = *reinterpret_cast<const u32x4*>(k && at < dim ? k + at : nothing);
+        }
       }
     }
   };
-  uint32_t vf[VR][NC][CW];
+  typedef uint32_t vword __attribute__((ext_vector_type(CW)));
+  vword vf[VR][NC];
   auto load_values = [&](const Place& p) {
 #pragma unroll
-    for (int y = 0; y < VR; ++y) {
-      const int b = y / 4, i = y % 4;
-      const T* v;
+    for (int b = 0; b < KB; ++b) {
       if constexpr (BLOCKS) {
-        v = vbase + (int64_t)max(p.page[b], 0) * a.c.v_stride[0] + (int64_t)p.slot[b] * vs;
-        v += (4 * g + i) * vs + CE * m;
-      } else {
-        const int from = 16 * b + 4 * g + i;
-        const int page = __shfl(p.page[0], from), slot = __shfl(p.slot[0], from);
-        v = vbase + (int64_t)max(page, 0) * a.c.v_stride[0] + (int64_t)slot * vs + CE * m;
-      }
+        const auto r = run(vbase, a.c.v_stride[0], vs, p, b);
 #pragma unroll
-      for (int part = 0; part < NC; ++part) {
-        const int at = 16 * CE * part;
-        if (at + CE * m < dim) {
-          if constexpr (CW == 4) {
-            const u32x4 w = *reinterpret_cast<const u32x4*>(v + at);
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int i2 = 0; i2 < 4; ++i2) vf[y][part][i2] = w[i2];
-          } else {
-            const u32x2 w = *reinterpret_cast<const u32x2*>(v + at);
-            vf[y][part][0] = w[0], vf[y][part][1] = w[1];
+          for (int part = 0; part < NC; ++part) {
+            if constexpr (CW == 4)
+              vf[4 * b + i][part] = __builtin_amdgcn_raw_buffer_load_b128(r, vo[i][part], 0, 0);
+            else
+              vf[4 * b + i][part] = __builtin_amdgcn_raw_buffer_load_b64(r, vo[i][part], 0, 0);
           }
-        } else {
+      } else {
 #pragma unroll
-          for (int i2 = 0; i2 < CW; ++i2) vf[y][part][i2] = 0;
+        for (int i = 0; i < 4; ++i) {
+          const T* v = one(vbase, a.c.v_stride[0], vs, p, 16 * b + 4 * g + i);
+#pragma unroll
+          for (int part = 0; part < NC; ++part) {
+            const int at = 16 * CE * part + CE * m;
+            vf[4 * b + i][part] = *reinterpret_cast<const vword*>(v && at < dim ? v + at : nothing);
+          }
         }
       }
     }
@@ -242,9 +277,15 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
     for (int e = 0; e < NC * CE; ++e) o[e] = f32x4{};
     top = -INFINITY, l = 0.0f;
     int block = block0 + wave;
-    Place now = locate(min(block, max(blocks - 1, 0)));
-    if (block < block1) load_keys(now), load_values(now);
-    Place next = locate(block + kWaves);
+#pragma unroll
+    for (int b = 0; b < RUNS; ++b) {
+      key[b] = block * KEYS + (BLOCKS ? 16 * b : lane & (KEYS - 1));
+      column[b] = (int)((uint32_t)key[b] / (uint32_t)size);
+      slot[b] = key[b] - column[b] * size;
+    }
+    // (pages are looked up before the loads of a step: loads return in order)
+    Place now = locate(), next = locate();
+    load_keys(now), load_values(now);
     for (; block < block1; block += kWaves) {
       const int j0 = block * KEYS;
       f32x4 s[KB];
@@ -260,14 +301,16 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
       if constexpr (BLOCKS) {
 #pragma unroll
         for (int b = 0; b < KB; ++b)
-          if (now.page[b] < 0) there &= ~(0xFu << (4 * b)), whole = false;
+          if (now.page[b] < 0 || now.page[b] >= a.c.pages)
+            there &= ~(0xFu << (4 * b)), whole = false;
       } else {
-        const uint64_t ok = __ballot(now.page[0] >= 0);
+        const uint64_t ok = __ballot(now.page[0] >= 0 && now.page[0] < a.c.pages);
         whole = ok == ~(uint64_t)0;
         there = (uint32_t)(ok >> (4 * g)) & 0xFu;
         if constexpr (KB == 2) there |= ((uint32_t)(ok >> (16 + 4 * g)) & 0xFu) << 4;
       }
-      if (block + kWaves < block1) load_keys(next);
+      const Place after = locate();
+      load_keys(next);
 
       const bool masked = !whole || j0 + KEYS > all_see;
 #pragma unroll
@@ -320,18 +363,6 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
         lo = __builtin_bit_cast(u32x4, d);
       }
 
-      // values of keys that are not there are left out, whatever they are
-      if (masked) {
-#pragma unroll
-        for (int y = 0; y < VR; ++y) {
-          const bool in = j0 + 16 * (y / 4) + 4 * g + y % 4 < t.length && (there >> y & 1);
-#pragma unroll
-          for (int part = 0; part < NC; ++part)
-#pragma unroll
-            for (int w = 0; w < CW; ++w)
-              if (!in) vf[y][part][w] = 0;
-        }
-      }
       if constexpr (decltype(with_wild)::value) {
         u32x4 see;
         if constexpr (HALF) {
@@ -348,9 +379,9 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
       } else {
         add_values(with_wild, hi, lo, u32x4{}, p[0]);
       }
-      if (block + kWaves < block1) load_values(next);
+      load_values(next);
       now = next;
-      next = locate(block + 2 * kWaves);
+      next = after;
     }
   };
   // A value that is not finite makes its product with any probability so, zeros of rows
@@ -420,10 +451,18 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
 template <typename T, int D>
 hipError_t launch_width(const AttentionArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)a.plan.tiles, (unsigned)a.plan.splits, (unsigned)a.c.heads);
-  if (a.c.page % 16 == 0)
-    k_attention_few<T, D, true><<<grid, 64 * kWaves, 0, stream>>>(a);
-  else
-    k_attention_few<T, D, false><<<grid, 64 * kWaves, 0, stream>>>(a);
+  const bool blocks = a.c.page % 16 == 0;
+  if (a.plan.wide) {
+    if (blocks)
+      k_attention_few<T, D, true, 8><<<grid, 512, 0, stream>>>(a);
+    else
+      k_attention_few<T, D, false, 8><<<grid, 512, 0, stream>>>(a);
+  } else {
+    if (blocks)
+      k_attention_few<T, D, true, 4><<<grid, 256, 0, stream>>>(a);
+    else
+      k_attention_few<T, D, false, 4><<<grid, 256, 0, stream>>>(a);
+  }
   return hipGetLastError();
 }
 

@@ -11,7 +11,7 @@ namespace {
 constexpr int64_t kMaxHeads = 65535;
 constexpr int64_t kMaxTokens = (int64_t(1) << 31) - 1;
 constexpr int64_t kMaxKeys = int64_t(1) << 30;      // of a sequence
-constexpr int64_t kMaxSlotStride = int64_t(1) << 26;
+constexpr int64_t kMaxSlotStride = int64_t(1) << 24;
 constexpr int64_t kMaxStride = int64_t(1) << 40;
 
 #define CACHE_TRY(expr)              \

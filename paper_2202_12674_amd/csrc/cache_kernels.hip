@@ -139,11 +139,15 @@ LSSVM_DEV void copy_chunk(const T* x, T* y, int at, int n) {
 
 // Heads that a thread handles one after the other with the same factors: as many as
 // leave `enough` threads, since a chunk's sines cost more than its 16 bytes, and a
-// few tokens need the threads more.
-constexpr int64_t kEnoughThreads = 256 * 1024;
-inline int heads_per_thread(int64_t tokens, int chunks, int heads) {
+// few tokens need the threads more. Rotation alone wants eight times what the chip
+// holds, to even out its end (16384 tokens x 32 heads x 128, 1/4, 1/2, 1 and 2 x 2^20
+// threads: 65, 51, 45 and 42 us); an appending thread first looks up where its token
+// goes, and half as many as the chip holds do best (9 x 2048 tokens x 8 heads x 128,
+// 1/4, 1/2, 1 and 2 x 2^20: 24, 23, 27 and 47 us).
+constexpr int64_t kRotaryThreads = 2 << 20, kAppendThreads = 1 << 19;
+inline int heads_per_thread(int64_t tokens, int chunks, int heads, int64_t enough) {
   const int64_t threads = tokens * chunks * heads;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(heads, threads / kEnoughThreads));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(heads, threads / enough));
 }
 
 // v / by and the rest; in 32 bits where they do.
@@ -411,7 +415,7 @@ hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream) {
     const bool in_place = a.x == a.out;
     const int chunks = turned + (in_place ? 0 : copy_chunks<T>(a.dim - 2 * a.pairs));
     if (chunks == 0) return hipSuccess;
-    const int each = heads_per_thread(a.tokens, chunks, a.heads);
+    const int each = heads_per_thread(a.tokens, chunks, a.heads, kRotaryThreads);
     const int groups = (a.heads + each - 1) / each;
     const int64_t items = a.tokens * groups * chunks;
     const dim3 grid((unsigned)((items + kThreads - 1) / kThreads));
@@ -429,7 +433,7 @@ hipError_t launch_append(const AppendArgs& a, hipStream_t stream) {
     const int turned = pair_chunks<T>(a.k.pairs, a.k.interleaved);
     const int copied = copy_chunks<T>(a.k.dim - 2 * a.k.pairs);
     const int chunks = turned + copied + copy_chunks<T>(a.k.dim);
-    const int each = heads_per_thread(a.k.tokens, chunks, a.k.heads);
+    const int each = heads_per_thread(a.k.tokens, chunks, a.k.heads, kAppendThreads);
     const int groups = (a.k.heads + each - 1) / each;
     const int64_t items = a.k.tokens * groups * chunks;
     const dim3 grid((unsigned)((items + kThreads - 1) / kThreads));
