@@ -37,6 +37,13 @@ LSSVM_DEV u32x4 load_loose(const T* p) {
   return __builtin_bit_cast(u32x4, *reinterpret_cast<const Loose<T, kVec<T>>*>(p));
 }
 
+// Keeps a value whole and in its registers here: the compiler else takes the results
+// apart between the steps and moves them all back every time.
+template <typename V>
+LSSVM_DEV void pin(V& v) {
+  asm volatile("" : "+v"(v));
+}
+
 // use(n, read(n)) for n < N, with the reads (of LDS) four ahead, in just this order: left
 // alone, the compiler waits for every read.
 template <int N, typename R, typename U>
@@ -335,6 +342,10 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
       int page = -1, slot = 0;
       if (mine) page = look_up(block + 2, &slot);
       if (block + 1 < block1) load(block + 1);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int b = 0; b < DB; ++b) pin(o[rb][b]);
       if (pass > 0) {   // in place, since only this step reads them
         for (int x = (int)threadIdx.x * 4; x < S::VBYTES; x += 256 * kWaves) {
           uint32_t* w = reinterpret_cast<uint32_t*>(&vt[buf][x]);
@@ -373,12 +384,16 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
               for (int i = 0; i < 16; ++i)
                 if (!sees(rb, 32 * b + result_row(i, 0))) s[rb][b][i] = -INFINITY;
           }
-          float high = s[rb][0][0];
+          float highs[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) highs[i] = s[rb][0][i];
 #pragma unroll
           for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) high = fmaxf(high, s[rb][b][i]);
-          high = max_across_32(high);
+            for (int i = b == 0 ? 4 : 0; i < 16; ++i)
+              highs[i % 4] = fmaxf(highs[i % 4], s[rb][b][i]);
+          const float high =
+              max_across_32(fmaxf(fmaxf(highs[0], highs[1]), fmaxf(highs[2], highs[3])));
           if (__any(high > top[rb])) {
             const float grown = fmaxf(top[rb], high);
             const float old =
@@ -390,15 +405,16 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
               if (!counts) o[rb][b] *= old;
           }
           const float base = top[rb] == -INFINITY ? 0.0f : -top[rb] * scale2;
-          float sum = 0.0f;
+          float sum[4] = {};
 #pragma unroll
           for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               s[rb][b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][b][i], scale2, base));
-              sum += s[rb][b][i];
+              sum[i % 4] += s[rb][b][i];
             }
-          l[rb] += sum;
+          l[rb] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          pin(l[rb]);
           if (counts) {
 #pragma unroll
             for (int b = 0; b < NB; ++b)
@@ -563,15 +579,27 @@ __global__ void __launch_bounds__(64 * kWaves) k_weights_chunk(AttentionArgs a) 
     const int first = max(0, j0 - (t.length - t.n)) * a.group / 32 * 32;
     row += first;
   }
-  for (; row < rows; row += 32 * kWaves) {
-    const int r = min(row + c, rows - 1), tok = r / a.group, head = hk * a.group + r % a.group;
-    const int lim = row + c < rows ? seen_keys(a, t, r) : 0;
-    const float lse = a.lse[(t.first + tok) * a.heads + head];
+  // a step's rows are read while the one before it is worked on
+  u32x4 qf[KC], qn[KC];
+  float lse, lse_n;
+  int lim, lim_n;
+  auto read = [&](int from) {
+    const int r = min(from + c, rows - 1), tok = r / a.group, head = hk * a.group + r % a.group;
+    lim_n = from + c < rows ? seen_keys(a, t, r) : 0;
+    lse_n = a.lse[(t.first + tok) * a.heads + head];
     const T* q = static_cast<const T*>(a.q) + (t.first + tok) * a.qs.outer + head * a.qs.head;
-    u32x4 qf[KC];
 #pragma unroll
-    for (int i = 0; i < KC; ++i)
-      qf[i] = 2 * i + h < chunks ? load_loose(q + (2 * i + h) * VE) : u32x4{};
+    for (int i = 0; i < KC; ++i) {   // (keys are zero behind the width)
+      const int at = min(2 * i + h, chunks - 1);
+      qn[i] = load_loose(q + at * VE);
+    }
+  };
+  if (rows > 0) read(row);
+  for (; row < rows; row += 32 * kWaves) {
+#pragma unroll
+    for (int i = 0; i < KC; ++i) qf[i] = qn[i];
+    lse = lse_n, lim = lim_n;
+    read(row + 32 * kWaves);
     const bool masked = j0 + 64 > seen_keys(a, t, row) || row + 32 > rows;
     const int left = lim - j0 - 4 * h;   // keys of this lane that its row sees
 #pragma unroll
@@ -579,10 +607,14 @@ __global__ void __launch_bounds__(64 * kWaves) k_weights_chunk(AttentionArgs a) 
       f32x16 z{};
 #pragma unroll
       for (int i = 0; i < KC; ++i) z = mul32<T>(kf[b][i], qf[i], z);
+      if (masked) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float p = __builtin_amdgcn_exp2f(z[i] * a.scale2 - lse);
-        sum[b][i] += masked && 32 * b + result_row(i, 0) >= left ? 0.0f : p;
+        for (int i = 0; i < 16; ++i)
+          if (32 * b + result_row(i, 0) < left)
+            sum[b][i] += __builtin_amdgcn_exp2f(z[i] * a.scale2 - lse);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[b][i] += __builtin_amdgcn_exp2f(z[i] * a.scale2 - lse);
       }
     }
   }
