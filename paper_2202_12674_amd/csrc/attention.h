@@ -47,8 +47,6 @@ constexpr int few_keys = sizeof(T) == 2 ? 32 : 16;
 template <typename T>
 constexpr int chunk_keys = sizeof(T) == 2 ? 64 : 32;
 constexpr int kFewLeast = 4, kChunkLeast = 4;
-constexpr int kChunkRB = 1;   // blocks of 32 rows per wave
-
 // ------------------------------------------------------------- device -------
 
 struct Tile {

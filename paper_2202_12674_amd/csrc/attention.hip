@@ -20,7 +20,7 @@ AttentionPlan make_plan(const lssvm_cache& c, int64_t tokens, int heads, bool ac
   AttentionPlan p{};
   const int64_t group = heads / c.heads, most = c.columns * c.page;
   p.few = tokens * group <= 32 * c.sequences;
-  p.rows = p.few ? 16 : 128 * kChunkRB;
+  p.rows = p.few ? 16 : 128;
   // every sequence's last tile may be partly empty
   p.tiles = tokens * group / p.rows + std::min(c.sequences, tokens);
   // Splits: enough workgroups for every CU to hold eight, which also evens out

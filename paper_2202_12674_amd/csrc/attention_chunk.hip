@@ -44,10 +44,11 @@ LSSVM_DEV void pin(V& v) {
   asm volatile("" : "+v"(v));
 }
 
-// use(n, read(n)) for n < N, with the reads (of LDS) four ahead, in just this order: left
-// alone, the compiler waits for every read.
-template <int N, typename R, typename U>
-LSSVM_DEV void read_ahead(R read, U use) {
+// use(n, read(n)) and side(n) for n < N, with the reads (of LDS) four ahead, in just
+// this order: left alone, the compiler waits for every read. `side` is vector work that
+// runs while the matrix cores are busy with `use`.
+template <int N, typename R, typename U, typename W>
+LSSVM_DEV void read_ahead(R read, U use, W side) {
   constexpr int AHEAD = N < 4 ? N : 4;
   decltype(read(0)) f[AHEAD];
 #pragma unroll
@@ -57,6 +58,7 @@ LSSVM_DEV void read_ahead(R read, U use) {
     __builtin_amdgcn_sched_barrier(0);
     use(n, f[n % AHEAD]);
     if (n + AHEAD < N) f[n % AHEAD] = read(n + AHEAD);
+    side(n);
   }
   __builtin_amdgcn_sched_barrier(0);
 }
@@ -117,8 +119,8 @@ struct Chunk {
 // go down 32 columns, writes down every eighth.
 LSSVM_DEV int column_at(int d, int keys8) { return d * 128 + 16 * (keys8 ^ ((d ^ (d >> 3)) & 7)); }
 
-// One tile of 128 RB rows against one split of its keys. A step's keys and values go
-// from memory into LDS past the registers, one step ahead, and every wave takes 32 RB
+// One tile of 128 rows against one split of its keys. A step's keys and values go
+// from memory into LDS past the registers, one step ahead, and every wave takes 32
 // rows over them: scores S^T = K Q^T, so that a row's scores are a lane's (and the
 // lane's 32 away); the running maximum and sum; and O^T += V^T P^T, whose operand P^T
 // the scores already are, register for register, if V^T's keys are taken in the same
@@ -127,8 +129,8 @@ LSSVM_DEV int column_at(int d, int keys8) { return d * 128 + 16 * (keys8 ^ ((d ^
 // in one piece; fp32 ones are read singly and stay in rows.
 // 16-bit types: p is rounded to the stored type for the product, half a step of it,
 // as the values themselves were; its sum is taken before that.
-template <typename T, int D, int RB>
-__global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
+template <typename T, int D>
+__global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
     k_attention_chunk(AttentionArgs a) {
   using S = Chunk<T, D>;
   constexpr int VE = S::VE, KEYS = S::KEYS, NB = S::NB, ROW = S::ROW, CH = S::CH, KC = S::KC,
@@ -149,7 +151,7 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
   const int64_t pair = work / a.plan.tiles;
   const int hk = (int)(pair / a.plan.splits), split = (int)(pair % a.plan.splits);
   Tile t;
-  if (!find_tile(a, work % a.plan.tiles, 32 * kWaves * RB, &t)) return;
+  if (!find_tile(a, work % a.plan.tiles, 32 * kWaves, &t)) return;
   const int per = split_blocks(t.keys, KEYS, a.plan.splits, kChunkLeast);
   const int blocks = (t.keys + KEYS - 1) / KEYS;
   const int used = max(1, (blocks + per - 1) / per);
@@ -163,24 +165,21 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
   const uint32_t sign = a.scale2 < 0.0f ? (HALF ? 0x80008000u : 0x80000000u) : 0;
   const uint32_t keep = a.scale2 == 0.0f ? 0 : ~0u;
   auto turned = [&](u32x4 q) { return (q ^ sign) & keep; };
-  u32x4 qf[RB][KC];
-  int lim[RB];
+  u32x4 qf[KC];
+  int lim;
   int all_see = t.length, some_see = 0;   // keys that every (any) row of the wave sees
+  const int y = wave * 32 + c, r = t.row0 + min(y, t.rows - 1);
+  lim = y < t.rows ? seen_keys(a, t, r) : 0;
+  const int tok = r / a.group, head = hk * a.group + r % a.group;
+  const T* q = static_cast<const T*>(a.q) + (t.first + tok) * a.qs.outer + head * a.qs.head;
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int y = wave * 32 * RB + 32 * rb + c, r = t.row0 + min(y, t.rows - 1);
-    lim[rb] = y < t.rows ? seen_keys(a, t, r) : 0;
-    const int tok = r / a.group, head = hk * a.group + r % a.group;
-    const T* q = static_cast<const T*>(a.q) + (t.first + tok) * a.qs.outer + head * a.qs.head;
-#pragma unroll
-    for (int k = 0; k < KC; ++k)
-      qf[rb][k] = 2 * k + h < chunks ? turned(load_loose(q + (2 * k + h) * VE)) : u32x4{};
-  }
+  for (int k = 0; k < KC; ++k)
+    qf[k] = 2 * k + h < chunks ? turned(load_loose(q + (2 * k + h) * VE)) : u32x4{};
   {
-    const int y = wave * 32 * RB;
+    const int y = wave * 32;
     if (y < t.rows) {
       all_see = seen_keys(a, t, t.row0 + y);
-      some_see = seen_keys(a, t, t.row0 + min(y + 32 * RB, t.rows) - 1);
+      some_see = seen_keys(a, t, t.row0 + min(y + 32, t.rows) - 1);
     }
   }
 
@@ -193,7 +192,7 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
     *reinterpret_cast<u32x4*>(&kt[0][x]) = u32x4{};
   for (int x = threadIdx.x * 16; x < 2 * S::VBYTES; x += 1024 * kWaves)
     *reinterpret_cast<u32x4*>(&vt[0][x]) = u32x4{};
-  constexpr uint64_t every = KEYS == 64 ? ~(uint64_t)0 : (uint64_t(1) << KEYS) - 1;
+  constexpr uint64_t every = ~(uint64_t)0 >> (64 - KEYS);
 
   // a lane's key of a step: looked up and, later, written down for all waves
   auto look_up = [&](int block, int* slot) {
@@ -300,8 +299,8 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
     }
   };
 
-  f32x16 o[RB][DB];
-  float top[RB], l[RB];
+  f32x16 o[DB];
+  float top, l;
 
   // Lane offsets of the 8 chunks (key and value) of a step, whose other parts are constant:
   // chunk 2x + h under the swizzle is 2x ^ (h ^ swizzle).
@@ -314,150 +313,159 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
 
   // One pass over the keys. Pass 0 is the only one unless values are not finite; the
   // others count only the values of one kind (below).
+  f32x16 s[NB];
+  float base;
   auto sweep = [&](int pass) {
     const Kind kind = (Kind)(pass - 1);
     const bool counts = pass > 1;
+    auto in_step = [&](int block) { return (block - block0) & 1; };
+    // scores: products of keys and queries, one block of 32 keys after the other
+    auto read_key = [&](int buf, int n) {
+      const int b = n / KC, k = n % KC;
+      return *reinterpret_cast<const u32x4*>(&kt[buf][ko[k % 4] + 32 * b * ROW + 128 * (k / 4)]);
+    };
+    auto score = [&](int n, u32x4 kf) {
+      const int b = n / KC, k = n % KC;
+      s[b] = mul32<T>(kf, qf[k], k == 0 ? f32x16{} : s[b]);
+    };
+    // four maxima of block b's scores
+    float highs[4];
+    auto look_at = [&](int b) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        highs[i % 4] = b == 0 && i < 4 ? s[b][i] : fmaxf(highs[i % 4], s[b][i]);
+    };
+    // masks the scores, brings the maximum and what hangs on it up to date. The maximum
+    // may stay up to 2^8 behind: p is then that much larger than 1.
+    auto settle = [&](int block) {
+      const int j0 = block * KEYS;
+      const uint64_t ok = there[(block - block0) & 3];
+      const uint64_t ok_h = ok >> (4 * h);   // of key k + 4 h
+      const int left = lim - j0 - 4 * h;
+      if (counts || (ok & every) != every || j0 + KEYS > all_see) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int k = 32 * b + result_row(i, 0);
+            const bool sees = k < left && (ok_h >> k & 1);
+            if (counts) s[b][i] = 0.0f;   // p = 1
+            if (!sees) s[b][i] = -INFINITY;
+          }
+          look_at(b);
+        }
+      } else {
+        look_at(NB - 1);
+      }
+      const float high =
+          max_across_32(fmaxf(fmaxf(highs[0], highs[1]), fmaxf(highs[2], highs[3])));
+      if (!counts && __any((high - top) * scale2 > 8.0f)) {
+        const float grown = fmaxf(top, high);
+        const float old =
+            __builtin_amdgcn_exp2f((top - (grown == -INFINITY ? 0.0f : grown)) * scale2);
+        top = grown;
+        l *= old;
+#pragma unroll
+        for (int b = 0; b < DB; ++b) {
+          o[b] *= old;
+          pin(o[b]);
+        }
+      }
+      base = counts || top == -INFINITY ? 0.0f : -top * scale2;
+    };
+    auto power = [&](int i) {   // p of score i
+      return __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 16][i % 16], scale2, base));
+    };
+    // 16-bit types: p in pairs, as the second product takes them
+    uint32_t pairs[HALF ? 8 * NB : 1];
+    auto make_pairs = [&](int from, int to) {
+      if constexpr (HALF) {
+        typedef T t2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int x = from; x < to; ++x) {
+          const float p = power(2 * x), q = power(2 * x + 1);
+          l += p + q;
+          pin(l);
+          pairs[x] = __builtin_bit_cast(uint32_t, t2{(T)p, (T)q});
+          pin(pairs[x]);
+        }
+      }
+    };
+    auto read_column = [&](int buf, int n) {
+      // (columns 32 apart differ in bit 2 of the swizzle)
+      const int step = n / DB, b = n % DB;
+      return *reinterpret_cast<const u32x4*>(&vt[buf][vo[step ^ (2 * (b & 1))] + 32 * 128 * b]);
+    };
+    auto add = [&](int n, u32x4 v) {
+      const int step = n / DB, b = n % DB;
+      const u32x4 p{pairs[4 * step], pairs[4 * step + 1], pairs[4 * step + 2],
+                    pairs[4 * step + 3]};
+      o[b] = mul32<T>(v, p, o[b]);
+    };
+    auto no_work = [](int) {};
+    auto only = [&](int buf) {   // values in place, since only this step reads them
+      for (int x = (int)threadIdx.x * 4; x < S::VBYTES; x += 256 * kWaves) {
+        uint32_t* w = reinterpret_cast<uint32_t*>(&vt[buf][x]);
+        *w = only_kind<T>(*w, kind);
+      }
+      __syncthreads();
+    };
+    constexpr int SCORES = KC * NB, SUMS = HALF ? KEYS / 16 * DB : 0;
+
     __syncthreads();   // the last pass has ended
+    top = -INFINITY, l = 0.0f;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      top[rb] = -INFINITY, l[rb] = 0.0f;
-#pragma unroll
-      for (int b = 0; b < DB; ++b) o[rb][b] = f32x16{};
-    }
+    for (int b = 0; b < DB; ++b) o[b] = f32x16{};
     if (wave < 2) {
       int slot = 0;
       const int page = look_up(block0 + wave, &slot);
       write_down(block0 + wave, page, slot);
     }
     __syncthreads();
-    if (block0 < block1) {
-      load(block0);
-      if constexpr (HALF) store_values(block0);
-    }
+    if (block0 >= block1) return;
+    load(block0);
+    if constexpr (HALF) store_values(block0);
+
     for (int block = block0; block < block1; ++block) {
-      const int buf = (block - block0) & 1, j0 = block * KEYS;
-      __builtin_amdgcn_s_waitcnt(0x0F70);   // this wave's loads have landed
-      __syncthreads();                      // ... and everyone's; the other buffers are free
+      const int buf = in_step(block);
+      __builtin_amdgcn_s_waitcnt(0x0F70);
+      __syncthreads();
       const bool mine = (block & (kWaves - 1)) == wave && block + 2 < block1;
       int page = -1, slot = 0;
       if (mine) page = look_up(block + 2, &slot);
       if (block + 1 < block1) load(block + 1);
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-        for (int b = 0; b < DB; ++b) pin(o[rb][b]);
-      if (pass > 0) {   // in place, since only this step reads them
-        for (int x = (int)threadIdx.x * 4; x < S::VBYTES; x += 256 * kWaves) {
-          uint32_t* w = reinterpret_cast<uint32_t*>(&vt[buf][x]);
-          *w = only_kind<T>(*w, kind);
-        }
-        __syncthreads();
-      }
-      if (j0 < some_see) {
-        f32x16 s[RB][NB];
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-          for (int rb = 0; rb < RB; ++rb) s[rb][b] = f32x16{};
-        read_ahead<KC * NB>(
-            [&](int n) {
-              const int b = n % NB, k = n / NB;
-              return *reinterpret_cast<const u32x4*>(
-                  &kt[buf][ko[k % 4] + 32 * b * ROW + 128 * (k / 4)]);
-            },
-            [&](int n, u32x4 kf) {
-#pragma unroll
-              for (int rb = 0; rb < RB; ++rb)
-                s[rb][n % NB] = mul32<T>(kf, qf[rb][n / NB], s[rb][n % NB]);
-            });
-        const uint64_t ok = there[(block - block0) & 3];
-        // whether this lane's row sees key k + 4 h of the step
-        const uint64_t ok_h = ok >> (4 * h);
-        auto sees = [&](int rb, int k) { return k < lim[rb] - j0 - 4 * h && (ok_h >> k & 1); };
-        const bool masked = (ok & every) != every || j0 + KEYS > all_see;
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          if (masked) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-              for (int i = 0; i < 16; ++i)
-                if (!sees(rb, 32 * b + result_row(i, 0))) s[rb][b][i] = -INFINITY;
-          }
-          float highs[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) highs[i] = s[rb][0][i];
-#pragma unroll
-          for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int i = b == 0 ? 4 : 0; i < 16; ++i)
-              highs[i % 4] = fmaxf(highs[i % 4], s[rb][b][i]);
-          const float high =
-              max_across_32(fmaxf(fmaxf(highs[0], highs[1]), fmaxf(highs[2], highs[3])));
-          if (__any(high > top[rb])) {
-            const float grown = fmaxf(top[rb], high);
-            const float old =
-                __builtin_amdgcn_exp2f((top[rb] - (grown == -INFINITY ? 0.0f : grown)) * scale2);
-            top[rb] = grown;
-            l[rb] *= old;
-#pragma unroll
-            for (int b = 0; b < DB; ++b)
-              if (!counts) o[rb][b] *= old;
-          }
-          const float base = top[rb] == -INFINITY ? 0.0f : -top[rb] * scale2;
-          float sum[4] = {};
-#pragma unroll
-          for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              s[rb][b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][b][i], scale2, base));
-              sum[i % 4] += s[rb][b][i];
-            }
-          l[rb] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-          pin(l[rb]);
-          if (counts) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-              for (int i = 0; i < 16; ++i)
-                s[rb][b][i] = sees(rb, 32 * b + result_row(i, 0)) ? 1.0f : 0.0f;
-          }
-        }
+      for (int b = 0; b < DB; ++b) pin(o[b]);
+      if (pass > 0) only(buf);
+      if (block * KEYS < some_see) {
+        // the first block's maximum while the second's scores are formed
+        read_ahead<SCORES>([&](int n) { return read_key(buf, n); },
+                           [&](int n, u32x4 kf) { score(n, kf); },
+                           [&](int n) {
+                             if (NB == 2 && n == KC) look_at(0);
+                           });
+        settle(block);
         if constexpr (HALF) {
-          typedef T t8 __attribute__((ext_vector_type(8)));
-          u32x4 p[RB];
-          read_ahead<KEYS / 16 * DB>(
-              [&](int n) {
-                // (columns 32 apart differ in bit 2 of the swizzle)
-                const int step = n / DB, b = n % DB;
-                return *reinterpret_cast<const u32x4*>(
-                    &vt[buf][vo[step ^ (2 * (b & 1))] + 32 * 128 * b]);
-              },
-              [&](int n, u32x4 v) {
-                const int step = n / DB, b = n % DB;
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb) {
-                  if (b == 0) {
-                    t8 x;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = (T)s[rb][step / 2][8 * (step % 2) + e];
-                    p[rb] = __builtin_bit_cast(u32x4, x);
-                  }
-                  o[rb][b] = mul32<T>(v, p[rb], o[rb][b]);
-                }
-              });
+          // the probabilities of 16 keys while those of the 16 before are multiplied
+          make_pairs(0, 4);
+          read_ahead<SUMS>([&](int n) { return read_column(buf, n); },
+                           [&](int n, u32x4 v) { add(n, v); },
+                           [&](int n) {
+                             const int step = n / DB + 1, b = n % DB;
+                             if (step < KEYS / 16)
+                               make_pairs(4 * step + 4 * b / DB, 4 * step + 4 * (b + 1) / DB);
+                           });
         } else {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int row = result_row(i, h);
+            const float p = power(i);
+            l += p;
 #pragma unroll
             for (int b = 0; b < DB; ++b) {
-              const uint32_t v = *reinterpret_cast<const uint32_t*>(
+              const float v = *reinterpret_cast<const float*>(
                   &vt[buf][row * ROW + 16 * ((8 * b + c / 4) ^ (row & S::TURN)) + 4 * (c % 4)]);
-#pragma unroll
-              for (int rb = 0; rb < RB; ++rb)
-                o[rb][b] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(v), s[rb][0][i],
-                                                                o[rb][b], 0, 0, 0);
+              o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p, o[b], 0, 0, 0);
             }
           }
         }
@@ -470,47 +478,44 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
   // writes the sums, or adds what values of `kind` make of them
   const int64_t rows = a.tokens * a.heads;
   auto write = [&](Kind kind) {
+    const int y = wave * 32 + c;
+    const float sum = l + __shfl_xor(l, 32);
+    if (y >= t.rows) return;
+    const int r = t.row0 + y, tok = r / a.group, head = hk * a.group + r % a.group;
+    const int64_t at = (t.first + tok) * a.heads + head;
+    T* out = static_cast<T*>(a.out) + (t.first + tok) * a.os.outer + head * a.os.head;
+    float* part = a.part + (split * rows + at) * dim;
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const int y = wave * 32 * RB + 32 * rb + c;
-      const float sum = l[rb] + __shfl_xor(l[rb], 32);
-      if (y >= t.rows) continue;
-      const int r = t.row0 + y, tok = r / a.group, head = hk * a.group + r % a.group;
-      const int64_t at = (t.first + tok) * a.heads + head;
-      T* out = static_cast<T*>(a.out) + (t.first + tok) * a.os.outer + head * a.os.head;
-      float* part = a.part + (split * rows + at) * dim;
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    for (int b = 0; b < DB; ++b)
 #pragma unroll
-      for (int b = 0; b < DB; ++b)
+      for (int i = 0; i < 16; i += 4) {
+        const int d = 32 * b + result_row(i, h);
+        if (d >= dim) continue;
+        f32x4 v{o[b][i], o[b][i + 1], o[b][i + 2], o[b][i + 3]};
+        if (kind != Kind::finite) {
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-          const int d = 32 * b + result_row(i, h);
-          if (d >= dim) continue;
-          f32x4 v{o[rb][b][i], o[rb][b][i + 1], o[rb][b][i + 2], o[rb][b][i + 3]};
-          if (kind != Kind::finite) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if (v[e] == 0.0f) continue;
-              if (used == 1)
-                out[d + e] = (T)((float)out[d + e] + wild_value(kind));
-              else
-                part[d + e] += wild_value(kind);
-            }
-          } else if (used == 1) {
-            Loose<T, 4> w;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w.v[e] = (T)(sum == 0.0f ? 0.0f : v[e] * inv);
-            *reinterpret_cast<Loose<T, 4>*>(out + d) = w;
-          } else {
-            *reinterpret_cast<f32x4*>(part + d) = v;
+          for (int e = 0; e < 4; ++e) {
+            if (v[e] == 0.0f) continue;
+            if (used == 1)
+              out[d + e] = (T)((float)out[d + e] + wild_value(kind));
+            else
+              part[d + e] += wild_value(kind);
           }
+        } else if (used == 1) {
+          Loose<T, 4> w;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w.v[e] = (T)(sum == 0.0f ? 0.0f : v[e] * inv);
+          *reinterpret_cast<Loose<T, 4>*>(out + d) = w;
+        } else {
+          *reinterpret_cast<f32x4*>(part + d) = v;
         }
-      if (kind == Kind::finite && h == 0) {
-        if (used > 1)
-          a.part_ml[split * rows + at] = float2{top[rb] * scale2, sum};
-        else if (a.lse)
-          a.lse[at] = sum == 0.0f ? INFINITY : top[rb] * scale2 + __builtin_amdgcn_logf(sum);
       }
+    if (kind == Kind::finite && h == 0) {
+      if (used > 1)
+        a.part_ml[split * rows + at] = float2{top * scale2, sum};
+      else if (a.lse)
+        a.lse[at] = sum == 0.0f ? INFINITY : top * scale2 + __builtin_amdgcn_logf(sum);
     }
   };
 
@@ -523,11 +528,9 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
     if (pass == 0) {
       int wild = 0;
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
         for (int b = 0; b < DB; ++b)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) wild |= !__builtin_isfinite(o[rb][b][i]);
+          for (int i = 0; i < 16; ++i) wild |= !__builtin_isfinite(o[b][i]);
       if (__syncthreads_or(wild)) continue;
     }
     write(pass == 0 ? Kind::finite : (Kind)(pass - 1));
@@ -539,7 +542,7 @@ __global__ void __launch_bounds__(64 * kWaves, D * RB > 128 ? 1 : 2)
 // registers: every wave takes every fourth 32 rows, forms the scores anew and sums
 // p = 2^(score - lse) per key; the waves' sums are joined in order.
 template <typename T, int D>
-__global__ void __launch_bounds__(64 * kWaves) k_weights_chunk(AttentionArgs a) {
+__global__ void __launch_bounds__(256) k_weights_chunk(AttentionArgs a) {
   using S = Chunk<T, D>;
   constexpr int VE = S::VE, KC = S::KC, NB = 2;
   __shared__ float sums[kWaves][64];
@@ -643,14 +646,14 @@ template <typename T, int D>
 hipError_t launch_width(const AttentionArgs& a, hipStream_t stream) {
   const int64_t count = a.plan.tiles * a.plan.splits * a.c.heads;
   const dim3 grid((unsigned)((count + 7) / 8 * 8));
-  k_attention_chunk<T, D, kChunkRB><<<grid, 64 * kWaves, 0, stream>>>(a);
+  k_attention_chunk<T, D><<<grid, 64 * kWaves, 0, stream>>>(a);
   return hipGetLastError();
 }
 template <typename T, int D>
 hipError_t weights_width(const AttentionArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)((a.c.columns * a.c.page + 63) / 64), (unsigned)a.c.heads,
                   (unsigned)a.c.sequences);
-  k_weights_chunk<T, D><<<grid, 64 * kWaves, 0, stream>>>(a);
+  k_weights_chunk<T, D><<<grid, 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
