@@ -91,7 +91,9 @@ LSSVM_DEV bool find_tile(const AttentionArgs& a, int64_t index, int rows, Tile* 
       const int at = __ffsll((unsigned long long)behind) - 1;
       const int64_t skipped = before + __shfl(to - mine, at);
       t->s = __builtin_amdgcn_readfirstlane(base + at);
-      t->first = __shfl(first, at);
+      first = __shfl(first, at);
+      t->first = (int64_t)__builtin_amdgcn_readfirstlane((int)(first >> 32)) << 32 |
+                 (uint32_t)__builtin_amdgcn_readfirstlane((int)first);
       t->n = __builtin_amdgcn_readfirstlane(__shfl(n, at));
       t->length = __builtin_amdgcn_readfirstlane(__shfl(length, at));
       t->row0 = __builtin_amdgcn_readfirstlane((int)(index - skipped) * rows);

@@ -11,9 +11,7 @@ hipError_t launch_weights_chunk(const AttentionArgs& a, hipStream_t stream);
 namespace {
 
 constexpr int64_t kCUs = 256;
-#ifndef WIDE_MAX
-#define WIDE_MAX 768
-#endif
+constexpr int64_t kWideKeys = 768;
 constexpr int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 
 AttentionPlan make_plan(const lssvm_cache& c, int64_t tokens, int heads, bool accumulate) {
@@ -23,14 +21,20 @@ AttentionPlan make_plan(const lssvm_cache& c, int64_t tokens, int heads, bool ac
   p.rows = p.few ? 16 : 128;
   // every sequence's last tile may be partly empty
   p.tiles = tokens * group / p.rows + std::min(c.sequences, tokens);
-  // Splits: enough workgroups for every CU to hold eight, which also evens out
-  // sequences of different lengths, but none of fewer than 128 keys.
+  // Splits: so many workgroups per CU, which also evens out sequences of different
+  // lengths, but none of fewer than 128 keys (joining costs a launch and what the parts
+  // take). Few rows: four, of wide heads, which fill the registers, two (64 x 16384
+  // keys x 128, 2, 4 and 8 per CU: 559, 566, 557 us; 16 x 4000 keys 43, 43, 49; 20 x
+  // 10000 keys x 256 103, 133, 179). Chunks: two, as many as a CU holds (1 x 512 rows
+  // over 8192 keys, 1, 2 and 4: 187, 116, 136 us; 2 x 2048 over 2048 98, 98, 114).
   const int64_t whole = std::max<int64_t>(1, std::max(tokens * group / p.rows,
                                                       std::min(c.sequences, tokens)) * c.heads);
-  const int64_t want = std::max<int64_t>(1, (p.few ? 8 : 2) * kCUs / whole);
+  const int64_t want = std::max<int64_t>(1, (p.few && c.dim <= 128 ? 4 : 2) * kCUs / whole);
   p.splits = (int)std::max<int64_t>(
       1, std::min<int64_t>({want, (most + 127) / 128, p.few ? 64 : 16}));
-  if (p.few && whole <= kCUs && most <= WIDE_MAX) {
+  // Short caches of few tiles: eight waves in place of four go over them whole, and
+  // nothing is to be joined (1 x 500 keys 11 us against 14, 1000 15 against 14).
+  if (p.few && whole <= kCUs && most <= kWideKeys) {
     p.wide = true;
     p.splits = 1;
   }
