@@ -20,6 +20,8 @@
  * negative one none; offsets count as if cut to [0, tokens]; a page number outside
  * [0, pages) is a hole, whose keys no row sees and which is never written.
  *
+ * Rows (tokens x heads) of one call are at most 2^30, their values at most 2^33.
+ *
  * dtype (of k, v, x, q and out) is LSSVM_F32, LSSVM_BF16 or LSSVM_F16. Sums, softmax
  * statistics, weights and rotation factors are fp32, angles fp64.
  */
@@ -52,8 +54,8 @@ typedef struct lssvm_cache {
     int64_t heads;           /* key/value heads, 1 .. 65535                       */
     int64_t page;            /* keys per page, >= 1                               */
     int64_t dim;             /* values per key and head, a multiple of 8, 8 .. 256 */
-    int64_t sequences;       /* 1 .. 65535                                        */
-    int64_t columns;         /* columns of table, >= 1; columns * page <= 2^30    */
+    int64_t sequences;       /* 1 .. 65535; sequences * heads <= 2^22             */
+    int64_t columns;         /* columns of table, >= 1; columns * page <= 2^29    */
     int64_t k_stride[3];     /* page, head, slot                                  */
     int64_t v_stride[3];     /* page, head, slot                                  */
     int64_t weight_stride[2]; /* page, head                                       */

@@ -10,7 +10,11 @@ namespace {
 
 constexpr int64_t kMaxHeads = 65535;
 constexpr int64_t kMaxTokens = (int64_t(1) << 31) - 1;
-constexpr int64_t kMaxKeys = int64_t(1) << 30;      // of a sequence
+// A launch's grid has less than 2^32 threads along each of its sides.
+constexpr int64_t kMaxKeys = int64_t(1) << 29;      // of a sequence
+constexpr int64_t kMaxRows = int64_t(1) << 30;      // tokens x heads
+constexpr int64_t kMaxValues = int64_t(1) << 33;    // ... x dim
+constexpr int64_t kMaxTables = int64_t(1) << 22;    // sequences x heads of a cache
 constexpr int64_t kMaxSlotStride = int64_t(1) << 24;
 constexpr int64_t kMaxStride = int64_t(1) << 40;
 
@@ -66,7 +70,8 @@ int check_cache(const lssvm_cache* c) {
       c->page < 1 || c->page > kMaxTokens || c->sequences < 1 || c->sequences > kMaxHeads)
     return bad("cache: pages, heads, page or sequences out of range");
   if (c->columns < 1 || c->columns > kMaxTokens || c->columns * c->page > kMaxKeys)
-    return bad("cache: columns * page must be 1 .. 2^30");
+    return bad("cache: columns * page must be 1 .. 2^29");
+  if (c->sequences * c->heads > kMaxTables) return bad("cache: more than 2^22 sequences x heads");
   if (c->table_stride < c->columns && c->sequences > 1)
     return bad("cache: table_stride must be at least columns");
   if (!aligned(c->k, 16) || !aligned(c->v, 16)) return bad("cache: k and v must be 16-byte aligned");
@@ -112,7 +117,8 @@ bool overlap(const void* a, const int64_t* as, const void* b, const int64_t* bs,
 int check_sizes(int64_t tokens, int64_t heads, int64_t dim) {
   if (tokens < 0 || tokens > kMaxTokens) return bad("tokens must be 0 .. 2^31 - 1");
   if (heads < 1 || heads > kMaxHeads) return bad("heads must be 1 .. 65535");
-  if ((double)tokens * heads * dim > 1e12) return bad("more than 10^12 values");
+  if (tokens * heads > kMaxRows || tokens * heads * dim > kMaxValues)
+    return bad("more than 2^30 rows (tokens x heads) or 2^33 values");
   return LSSVM_OK;
 }
 

@@ -42,7 +42,9 @@ def test_library_exports_every_declared_function():
 BAD_CACHES = [dict(k=None), dict(v=None), dict(table=None), dict(lengths=None), dict(dtype=0),
               dict(dtype=9), dict(dim=0), dict(dim=12), dict(dim=264), dict(pages=0),
               dict(pages=1 << 31), dict(heads=0), dict(heads=65536), dict(page=0),
-              dict(sequences=0), dict(sequences=65536), dict(columns=0), dict(columns=1 << 28),
+              dict(sequences=0), dict(sequences=65536), dict(columns=0), dict(columns=1 << 28), dict(sequences=65535, heads=65, k_stride=(66560, 1024, 64),
+                                                   v_stride=(66560, 1024, 64),
+                                                   weight_stride=(1040, 16)),
               dict(table_stride=3), dict(k=FAKE + 8), dict(v=FAKE + 2),
               dict(k_stride=(2048, 1024, 60)), dict(v_stride=(2044, 1024, 64)),
               dict(k_stride=(0, 1024, 64)), dict(k_stride=(2048, 1024, 32)),
@@ -93,7 +95,7 @@ def test_attention_refusals():
 
     for change in (dict(q=None), dict(qs=None), dict(out=None), dict(os=None), dict(offsets=None),
                    dict(tokens=-1), dict(tokens=1 << 31), dict(heads=0), dict(heads=3),
-                   dict(heads=65536), dict(scale=math.inf), dict(scale=math.nan), dict(ws=None),
+                   dict(heads=65536), dict(tokens=1 << 29), dict(scale=math.inf), dict(scale=math.nan), dict(ws=None),
                    dict(ws=two(16, 16)), dict(os=two(64, 64)), dict(os=two(256, 32)),
                    dict(os=two(-256, 64)), dict(q=FAKE + 1), dict(out=2 * FAKE + 1),
                    dict(out=FAKE), dict(out=FAKE + 1024), dict(work=None), dict(work=FAKE + 8),
@@ -122,7 +124,7 @@ def test_rotary_refusals():
                    dict(bytes=2), dict(pos=FAKE + 4), dict(freqs=None), dict(freqs=FAKE + 4),
                    dict(scale=math.inf), dict(dtype=0), dict(dtype=7), dict(os=two(64, 64)),
                    dict(x=FAKE + 1), dict(out=FAKE + 64), dict(out=FAKE, os=two(512, 64)),
-                   dict(tokens=1 << 30, heads=1 << 15)):
+                   dict(tokens=1 << 30, heads=1 << 15), dict(tokens=1 << 20, heads=1 << 10, dim=64)):
         assert call(**change) == B.EINVAL, change
     assert call(tokens=0, x=None, out=None, pos=None) == B.OK
 

@@ -461,13 +461,13 @@ def test_a_prompt_tokens_and_an_eviction(torch_dev, dtype):
     step([20, 1])
 
 
-@pytest.mark.parametrize("new", [1, 70])
-def test_a_captured_step_replays(torch_dev, new):
+@pytest.mark.parametrize("new,longest", [(1, 333), (70, 333), (1, 20000)])
+def test_a_captured_step_replays(torch_dev, new, longest):
     """Append, attention with weights and eviction in one graph, replayed with eager
     work between: every replay as the eager calls."""
     torch, dev = torch_dev
     import paper_2202_12674_amd as P
-    cache, _ = make(torch, dev, "bf16", [200, 333], 2, 64, 16, 3)
+    cache, _ = make(torch, dev, "bf16", [200, longest], 2, 64, 16, 3)
     target, _ = make(torch, dev, "bf16", [128, 128], 2, 64, 16, 4)
     off = offsets_of(torch, [new, new]).to(dev)
     f, _ = P.rotary_frequencies(64, device=dev)
@@ -500,6 +500,45 @@ def test_a_captured_step_replays(torch_dev, new):
         torch.cuda.synchronize()
         assert torch.equal(got, y) and torch.equal(kept, want), i
         assert torch.equal(wout.nan_to_num(-1), w.nan_to_num(-1)), i
+
+
+def test_two_captured_graphs_share_a_workspace(torch_dev):
+    """Two captured calls of other sizes that use one workspace, replayed in turn: a call
+    reads nothing there that it has not written."""
+    torch, dev = torch_dev
+    import paper_2202_12674_amd as P
+    parts = []
+    for new, lengths in ((1, [900, 40]), (60, [300, 77])):
+        cache, _ = make(torch, dev, "f16", lengths, 2, 64, 16, new)
+        parts.append((cache, offsets_of(torch, [new, new]).to(dev),
+                      torch.randn(2 * new, 8, 64, device=dev).half(),
+                      torch.zeros(cache.weight.shape, device=dev)))
+    ws = P.alloc_workspace(max(P.attention_workspace_bytes(c, q.shape[0], 8, True)
+                               for c, _, q, _ in parts), dev)
+
+    def step(c, off, q, w):
+        return P.attention(q, c, off, accumulate=True, weight_out=w, workspace=ws)
+
+    want = []
+    for p in parts:
+        want.append((step(*p).clone(), p[3].clone()))
+    graphs, got = [], []
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for p in parts:
+            step(*p)
+    side.synchronize()
+    for p in parts:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            got.append(step(*p))
+        graphs.append(g)
+    for i in (0, 1, 1, 0, 1, 0):
+        got[i].zero_(), parts[i][3].zero_(), ws.fill_(255)
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got[i], want[i][0])
+        assert torch.equal(parts[i][3].nan_to_num(-1), want[i][1].nan_to_num(-1))
 
 
 def test_results_do_not_depend_on_the_run(torch_dev):
