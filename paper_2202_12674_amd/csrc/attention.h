@@ -129,6 +129,16 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+// Zeros, for loads that have nothing else to load.
+static __device__ const u32x4 kNothing[1] = {};
+
+// A load that is known to be from global memory, where the compiler cannot tell.
+template <typename V, typename T>
+LSSVM_DEV V load_global(const T* p) {
+  return *reinterpret_cast<const __attribute__((address_space(1))) V*>(
+      reinterpret_cast<uintptr_t>(p));
+}
+
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 

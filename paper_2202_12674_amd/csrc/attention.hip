@@ -26,10 +26,12 @@ AttentionPlan make_plan(const lssvm_cache& c, int64_t tokens, int heads, bool ac
   // take). Few rows: four, of wide heads, which fill the registers, two (64 x 16384
   // keys x 128, 2, 4 and 8 per CU: 559, 566, 557 us; 16 x 4000 keys 43, 43, 49; 20 x
   // 10000 keys x 256 103, 133, 179). Chunks: two, as many as a CU holds (1 x 512 rows
-  // over 8192 keys, 1, 2 and 4: 187, 116, 136 us; 2 x 2048 over 2048 98, 98, 114).
+  // over 8192 keys, 1, 2 and 4: 187, 116, 136 us; 2 x 2048 over 2048 98, 98, 114); in
+  // fp32 one, which the matrix cores are busy with (3 x 300 over 2500, 1 and 2: 91, 97).
+  const int per_cu = p.few ? (c.dim <= 128 ? 4 : 2) : c.dtype == LSSVM_F32 ? 1 : 2;
   const int64_t whole = std::max<int64_t>(1, std::max(tokens * group / p.rows,
                                                       std::min(c.sequences, tokens)) * c.heads);
-  const int64_t want = std::max<int64_t>(1, (p.few && c.dim <= 128 ? 4 : 2) * kCUs / whole);
+  const int64_t want = std::max<int64_t>(1, per_cu * kCUs / whole);
   p.splits = (int)std::max<int64_t>(
       1, std::min<int64_t>({want, (most + 127) / 128, p.few ? 64 : 16}));
   // Short caches of few tiles: eight waves in place of four go over them whole, and

@@ -6,6 +6,7 @@ namespace lssvm {
 namespace {
 
 constexpr int kWaves = 4;
+constexpr int kWeightBlocks = 2;   // of 32 keys that a workgroup sums the weights of
 
 typedef __attribute__((address_space(1))) void* gptr_t;
 typedef __attribute__((address_space(3))) void* lptr_t;
@@ -136,8 +137,18 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
   constexpr int VE = S::VE, KEYS = S::KEYS, NB = S::NB, ROW = S::ROW, CH = S::CH, KC = S::KC,
                 DB = S::DB, LOADS = S::LOADS, VU = S::VU;
   constexpr bool HALF = S::HALF;
-  __shared__ __attribute__((aligned(16))) char kt[2][KEYS * ROW];
-  __shared__ __attribute__((aligned(16))) char vt[2][S::VBYTES];
+  // two buffers, as objects of their own: the compiler holds reads of the one only then
+  // apart from loads into the other, and else waits for those before every read
+  __shared__ __attribute__((aligned(16))) char kt0[KEYS * ROW], kt1[KEYS * ROW];
+  __shared__ __attribute__((aligned(16))) char vt0[S::VBYTES], vt1[S::VBYTES];
+  auto kt = [&](auto buf) -> char(&)[KEYS * ROW] {
+    if constexpr (buf == 0) return kt0; else return kt1;
+  };
+  auto vt = [&](auto buf) -> char(&)[S::VBYTES] {
+    if constexpr (buf == 0) return vt0; else return vt1;
+  };
+  constexpr std::integral_constant<int, 0> even{};
+  constexpr std::integral_constant<int, 1> odd{};
   __shared__ int64_t key_at[4][KEYS], value_at[4][KEYS];   // rows of a step, -1: none
   __shared__ uint64_t there[4];
 
@@ -186,103 +197,69 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
   const T* kbase = static_cast<const T*>(a.c.k) + hk * a.c.k_stride[1];
   const T* vbase = static_cast<const T*>(a.c.v) + hk * a.c.v_stride[1];
 
-  // LDS starts out as zeros: chunks behind the width stay so, which makes them count
-  // nothing, and keys that are not there are at worst old ones, whose scores are left out
-  for (int x = threadIdx.x * 16; x < 2 * KEYS * ROW; x += 1024 * kWaves)
-    *reinterpret_cast<u32x4*>(&kt[0][x]) = u32x4{};
-  for (int x = threadIdx.x * 16; x < 2 * S::VBYTES; x += 1024 * kWaves)
-    *reinterpret_cast<u32x4*>(&vt[0][x]) = u32x4{};
   constexpr uint64_t every = ~(uint64_t)0 >> (64 - KEYS);
 
-  // a lane's key of a step: looked up and, later, written down for all waves
-  auto look_up = [&](int block, int* slot) {
-    const int j = block * KEYS + (lane & (KEYS - 1));
-    return j < t.length ? cache_page(a.c, t.s, j, slot) : -1;
+  // a lane's key of a step: its page is looked up and, later, checked and written down
+  // for all waves
+  auto look_up = [&](int block) {
+    const int j = min(block * KEYS + (lane & (KEYS - 1)), t.length - 1);
+    return a.c.table[t.s * a.c.table_stride + (uint32_t)j / (uint32_t)a.c.page];
   };
-  auto write_down = [&](int block, int page, int slot) {
-    const int at = (block - block0) & 3;
+  auto write_down = [&](int block, int page) {
+    const int at = (block - block0) & 3, j = block * KEYS + (lane & (KEYS - 1));
+    const int slot = (int)((uint32_t)j % (uint32_t)a.c.page);
+    const bool ok = j < t.length && page >= 0 && page < a.c.pages;
     if (lane < KEYS) {
-      key_at[at][lane] = page < 0 ? -1 : page * a.c.k_stride[0] + slot * a.c.k_stride[2];
-      value_at[at][lane] = page < 0 ? -1 : page * a.c.v_stride[0] + slot * a.c.v_stride[2];
+      key_at[at][lane] = ok ? page * a.c.k_stride[0] + slot * a.c.k_stride[2] : -1;
+      value_at[at][lane] = ok ? page * a.c.v_stride[0] + slot * a.c.v_stride[2] : -1;
     }
-    const uint64_t ok = __ballot(page >= 0);
-    if (lane == 0) there[at] = ok;
+    const uint64_t all = __ballot(ok);
+    if (lane == 0) there[at] = all;
   };
+  // Keys that are not there and chunks behind the width are loaded as zeros from a place
+  // of their own: a load behind a branch would be waited for at its end.
+  const T* nothing = reinterpret_cast<const T*>(kNothing);
   // 16-bit values on their way: unit x of a step is chunk x % (D / 8) of the 4 keys from
   // 4 (x / (D / 8))
-  u32x4 vr[HALF ? VU : 1][4] = {};
-  auto load = [&](int block) {
-    const int at = (block - block0) & 3, buf = (block - block0) & 1;
-    const bool whole = (there[at] & every) == every;
+  u32x4 vr[HALF ? VU : 1][4];
+  auto load = [&](int block, auto buf) {
+    const int at = (block - block0) & 3;
     const int row = threadIdx.x / CH, place = threadIdx.x % CH;   // and 256 / CH rows on
-    constexpr int NEXT = S::NEXT;
     const int kc = place ^ (row & S::TURN);
-    int64_t ka[LOADS], va[LOADS];
-#pragma unroll
-    for (int u = 0; u < LOADS; ++u) ka[u] = key_at[at][row + u * NEXT];
     if constexpr (HALF) {
 #pragma unroll
       for (int u = 0; u < VU; ++u) {
         const int x = u * 64 * kWaves + (int)threadIdx.x, ch = x % (D / VE), kg = x / (D / VE);
-        int64_t at4[4];
+        int64_t from[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) at4[i] = value_at[at][(4 * kg + i) & (KEYS - 1)];
-        const bool in = ch < chunks && x < S::VUNITS;
-        if (whole) {
-          if (in) {
+        for (int i = 0; i < 4; ++i) from[i] = value_at[at][(4 * kg + i) & (KEYS - 1)];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              vr[u][i] = *reinterpret_cast<const u32x4*>(vbase + at4[i] + ch * VE);
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            vr[u][i] = u32x4{};
-            if (in && at4[i] >= 0)
-              vr[u][i] = *reinterpret_cast<const u32x4*>(vbase + at4[i] + ch * VE);
-          }
-        }
+        for (int i = 0; i < 4; ++i)
+          vr[u][i] = load_global<u32x4>(
+              from[i] >= 0 && ch < chunks ? vbase + from[i] + ch * VE : nothing);
       }
-    } else {
-#pragma unroll
-      for (int u = 0; u < LOADS; ++u) va[u] = value_at[at][row + u * NEXT];
     }
-    if (whole) {
-      if (kc < chunks) {
+    int64_t from[LOADS];
 #pragma unroll
-        for (int u = 0; u < LOADS; ++u)
-          __builtin_amdgcn_global_load_lds((gptr_t)(kbase + ka[u] + kc * VE),
-                                           (lptr_t)(&kt[buf][(u * kWaves + wave) * 1024]), 16, 0,
-                                           0);
-      }
-      if constexpr (!HALF) {
-        if (kc < chunks) {
+    for (int u = 0; u < LOADS; ++u) from[u] = key_at[at][row + u * S::NEXT];
 #pragma unroll
-          for (int u = 0; u < LOADS; ++u)
-            __builtin_amdgcn_global_load_lds((gptr_t)(vbase + va[u] + kc * VE),
-                                             (lptr_t)(&vt[buf][(u * kWaves + wave) * 1024]), 16,
-                                             0, 0);
-        }
-      }
-    } else {
+    for (int u = 0; u < LOADS; ++u) {
+      const T* k = from[u] >= 0 && kc < chunks ? kbase + from[u] + kc * VE : nothing;
+      __builtin_amdgcn_global_load_lds((gptr_t)k, (lptr_t)(&kt(buf)[(u * kWaves + wave) * 1024]),
+                                       16, 0, 0);
+    }
+    if constexpr (!HALF) {
+#pragma unroll
+      for (int u = 0; u < LOADS; ++u) from[u] = value_at[at][row + u * S::NEXT];
 #pragma unroll
       for (int u = 0; u < LOADS; ++u) {
-        const int first = (u * kWaves + wave) * 1024;   // wave-uniform
-        if (ka[u] >= 0 && kc < chunks)
-          __builtin_amdgcn_global_load_lds((gptr_t)(kbase + ka[u] + kc * VE),
-                                           (lptr_t)(&kt[buf][first]), 16, 0, 0);
-        if constexpr (!HALF) {
-          if (va[u] >= 0 && kc < chunks)
-            __builtin_amdgcn_global_load_lds((gptr_t)(vbase + va[u] + kc * VE),
-                                             (lptr_t)(&vt[buf][first]), 16, 0, 0);
-          else
-            *reinterpret_cast<u32x4*>(&vt[buf][first + lane * 16]) = u32x4{};
-        }
+        const T* v = from[u] >= 0 && kc < chunks ? vbase + from[u] + kc * VE : nothing;
+        __builtin_amdgcn_global_load_lds(
+            (gptr_t)v, (lptr_t)(&vt(buf)[(u * kWaves + wave) * 1024]), 16, 0, 0);
       }
     }
   };
-  auto store_values = [&](int block) {
-    const int buf = (block - block0) & 1;
+  auto store_values = [&](auto buf) {
 #pragma unroll
     for (int u = 0; u < VU; ++u) {
       const int x = u * 64 * kWaves + (int)threadIdx.x, ch = x % (D / VE), kg = x / (D / VE);
@@ -294,7 +271,7 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
         const uint32_t pick = e & 1 ? 0x07060302u : 0x05040100u;
         const u32x2 w{__builtin_amdgcn_perm(vr[u][1][e / 2], vr[u][0][e / 2], pick),
                       __builtin_amdgcn_perm(vr[u][3][e / 2], vr[u][2][e / 2], pick)};
-        *reinterpret_cast<u32x2*>(&vt[buf][column_at(8 * ch + e, keys8) + 8 * y]) = w;
+        *reinterpret_cast<u32x2*>(&vt(buf)[column_at(8 * ch + e, keys8) + 8 * y]) = w;
       }
     }
   };
@@ -318,11 +295,10 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
   auto sweep = [&](int pass) {
     const Kind kind = (Kind)(pass - 1);
     const bool counts = pass > 1;
-    auto in_step = [&](int block) { return (block - block0) & 1; };
     // scores: products of keys and queries, one block of 32 keys after the other
-    auto read_key = [&](int buf, int n) {
+    auto read_key = [&](auto buf, int n) {
       const int b = n / KC, k = n % KC;
-      return *reinterpret_cast<const u32x4*>(&kt[buf][ko[k % 4] + 32 * b * ROW + 128 * (k / 4)]);
+      return *reinterpret_cast<const u32x4*>(&kt(buf)[ko[k % 4] + 32 * b * ROW + 128 * (k / 4)]);
     };
     auto score = [&](int n, u32x4 kf) {
       const int b = n / KC, k = n % KC;
@@ -391,10 +367,10 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
         }
       }
     };
-    auto read_column = [&](int buf, int n) {
+    auto read_column = [&](auto buf, int n) {
       // (columns 32 apart differ in bit 2 of the swizzle)
       const int step = n / DB, b = n % DB;
-      return *reinterpret_cast<const u32x4*>(&vt[buf][vo[step ^ (2 * (b & 1))] + 32 * 128 * b]);
+      return *reinterpret_cast<const u32x4*>(&vt(buf)[vo[step ^ (2 * (b & 1))] + 32 * 128 * b]);
     };
     auto add = [&](int n, u32x4 v) {
       const int step = n / DB, b = n % DB;
@@ -403,9 +379,9 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
       o[b] = mul32<T>(v, p, o[b]);
     };
     auto no_work = [](int) {};
-    auto only = [&](int buf) {   // values in place, since only this step reads them
+    auto only = [&](auto buf) {   // values in place, since only this step reads them
       for (int x = (int)threadIdx.x * 4; x < S::VBYTES; x += 256 * kWaves) {
-        uint32_t* w = reinterpret_cast<uint32_t*>(&vt[buf][x]);
+        uint32_t* w = reinterpret_cast<uint32_t*>(&vt(buf)[x]);
         *w = only_kind<T>(*w, kind);
       }
       __syncthreads();
@@ -416,24 +392,18 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
     top = -INFINITY, l = 0.0f;
 #pragma unroll
     for (int b = 0; b < DB; ++b) o[b] = f32x16{};
-    if (wave < 2) {
-      int slot = 0;
-      const int page = look_up(block0 + wave, &slot);
-      write_down(block0 + wave, page, slot);
-    }
-    __syncthreads();
     if (block0 >= block1) return;
-    load(block0);
-    if constexpr (HALF) store_values(block0);
+    if (wave < 2) write_down(block0 + wave, look_up(block0 + wave));
+    __syncthreads();
+    load(block0, even);
+    if constexpr (HALF) store_values(even);
 
-    for (int block = block0; block < block1; ++block) {
-      const int buf = in_step(block);
+    auto step = [&](int block, auto buf, auto other) {
       __builtin_amdgcn_s_waitcnt(0x0F70);
       __syncthreads();
       const bool mine = (block & (kWaves - 1)) == wave && block + 2 < block1;
-      int page = -1, slot = 0;
-      if (mine) page = look_up(block + 2, &slot);
-      if (block + 1 < block1) load(block + 1);
+      const int page = look_up(block + 2);   // (by all: it is not waited for here)
+      if (block + 1 < block1) load(block + 1, other);
 #pragma unroll
       for (int b = 0; b < DB; ++b) pin(o[b]);
       if (pass > 0) only(buf);
@@ -464,15 +434,19 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
 #pragma unroll
             for (int b = 0; b < DB; ++b) {
               const float v = *reinterpret_cast<const float*>(
-                  &vt[buf][row * ROW + 16 * ((8 * b + c / 4) ^ (row & S::TURN)) + 4 * (c % 4)]);
+                  &vt(buf)[row * ROW + 16 * ((8 * b + c / 4) ^ (row & S::TURN)) + 4 * (c % 4)]);
               o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p, o[b], 0, 0, 0);
             }
           }
         }
       }
       if constexpr (HALF)
-        if (block + 1 < block1) store_values(block + 1);
-      if (mine) write_down(block + 2, page, slot);
+        if (block + 1 < block1) store_values(other);
+      if (mine) write_down(block + 2, page);
+    };
+    for (int block = block0; block < block1; block += 2) {
+      step(block, even, odd);
+      if (block + 1 < block1) step(block + 1, odd, even);
     }
   };
   // writes the sums, or adds what values of `kind` make of them
@@ -544,8 +518,8 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
 template <typename T, int D>
 __global__ void __launch_bounds__(256) k_weights_chunk(AttentionArgs a) {
   using S = Chunk<T, D>;
-  constexpr int VE = S::VE, KC = S::KC, NB = 2;
-  __shared__ float sums[kWaves][64];
+  constexpr int VE = S::VE, KC = S::KC, NB = kWeightBlocks;
+  __shared__ float sums[kWaves][32 * NB];
   const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int s = blockIdx.z, hk = blockIdx.y, chunks = (int)a.c.dim / VE;
@@ -553,7 +527,7 @@ __global__ void __launch_bounds__(256) k_weights_chunk(AttentionArgs a) {
   t.s = s;
   t.length = cache_length(a.c, s);
   sequence_rows(a, s, &t.first, &t.n);
-  const int j0 = blockIdx.x * 64, rows = t.n * a.group;
+  const int j0 = blockIdx.x * 32 * NB, rows = t.n * a.group;
   if (j0 >= t.length) return;
 
   u32x4 kf[NB][KC];
@@ -603,7 +577,7 @@ __global__ void __launch_bounds__(256) k_weights_chunk(AttentionArgs a) {
     for (int i = 0; i < KC; ++i) qf[i] = qn[i];
     lse = lse_n, lim = lim_n;
     read(row + 32 * kWaves);
-    const bool masked = j0 + 64 > seen_keys(a, t, row) || row + 32 > rows;
+    const bool masked = j0 + 32 * NB > seen_keys(a, t, row) || row + 32 > rows;
     const int left = lim - j0 - 4 * h;   // keys of this lane that its row sees
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -631,7 +605,7 @@ __global__ void __launch_bounds__(256) k_weights_chunk(AttentionArgs a) {
     }
   __syncthreads();
   const int j = j0 + (int)threadIdx.x;
-  if (threadIdx.x >= 64 || j >= t.length) return;
+  if (threadIdx.x >= 32 * NB || j >= t.length) return;
   int slot;
   const int page = cache_page(a.c, s, j, &slot);
   if (page < 0) return;
@@ -651,7 +625,7 @@ hipError_t launch_width(const AttentionArgs& a, hipStream_t stream) {
 }
 template <typename T, int D>
 hipError_t weights_width(const AttentionArgs& a, hipStream_t stream) {
-  const dim3 grid((unsigned)((a.c.columns * a.c.page + 63) / 64), (unsigned)a.c.heads,
+  const dim3 grid((unsigned)((a.c.columns * a.c.page + 32 * kWeightBlocks - 1) / (32 * kWeightBlocks)), (unsigned)a.c.heads,
                   (unsigned)a.c.sequences);
   k_weights_chunk<T, D><<<grid, 256, 0, stream>>>(a);
   return hipGetLastError();

@@ -10,7 +10,6 @@ namespace {
 // Third word of a raw buffer resource (32-bit data, no swizzle, no stride).
 constexpr int kBufferWord3 = 0x00020000;
 typedef const __attribute__((address_space(4))) int32_t* const_i32;
-__device__ const u32x4 kNothing[1] = {};
 
 // The matrix cores on 16 keys x 16 rows.
 template <typename T>
@@ -184,7 +183,7 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
 #pragma unroll
         for (int c = 0; c < KC; ++c) {
           const int at = (4 * c + g) * VE;
-          kf[b][c] = *reinterpret_cast<const u32x4*>(k && at < dim ? k + at : nothing);
+          kf[b][c] = load_global<u32x4>(k && at < dim ? k + at : nothing);
         }
       }
     }
@@ -212,7 +211,7 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
 #pragma unroll
           for (int part = 0; part < NC; ++part) {
             const int at = 16 * CE * part + CE * m;
-            vf[4 * b + i][part] = *reinterpret_cast<const vword*>(v && at < dim ? v + at : nothing);
+            vf[4 * b + i][part] = load_global<vword>(v && at < dim ? v + at : nothing);
           }
         }
       }
