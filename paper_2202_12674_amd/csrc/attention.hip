@@ -11,6 +11,7 @@ hipError_t launch_weights_chunk(const AttentionArgs& a, hipStream_t stream);
 namespace {
 
 constexpr int64_t kCUs = 256;
+constexpr int kMostSplits = 64;
 constexpr int64_t kWideKeys = 768;
 constexpr int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 
@@ -33,7 +34,7 @@ AttentionPlan make_plan(const lssvm_cache& c, int64_t tokens, int heads, bool ac
                                                       std::min(c.sequences, tokens)) * c.heads);
   const int64_t want = std::max<int64_t>(1, per_cu * kCUs / whole);
   p.splits = (int)std::max<int64_t>(
-      1, std::min<int64_t>({want, (most + 127) / 128, p.few ? 64 : 16}));
+      1, std::min<int64_t>({want, (most + 127) / 128, p.few ? kMostSplits : 16}));
   // Short caches of few tiles: eight waves in place of four go over them whole, and
   // nothing is to be joined (1 x 500 keys 11 us against 14, 1000 15 against 14).
   if (p.few && whole <= kCUs && most <= kWideKeys) {
@@ -76,23 +77,40 @@ __global__ void __launch_bounds__(256) k_attention_join(AttentionArgs a, int blo
   const int used = ((t.keys + block - 1) / block + per - 1) / per;
   if (used <= 1) return;
   const int hk = blockIdx.y, dim = (int)a.c.dim, quads = dim / 4, y0 = 16 * blockIdx.z;
+  const int here = min(16, t.rows - y0);
   const int64_t rows = a.tokens * a.heads;
-  for (int x = threadIdx.x; x < min(16, t.rows - y0) * quads; x += 256) {
-    const int y = y0 + x / quads, d = x % quads * 4;
-    const int tok = (t.row0 + y) / a.group, h = hk * a.group + (t.row0 + y) % a.group;
-    const int64_t at = (t.first + tok) * a.heads + h;
-    float m = -INFINITY;
-    for (int i = 0; i < used; ++i) m = fmaxf(m, a.part_ml[i * rows + at].x);
+  auto row = [&](int y) {
+    const int r = t.row0 + y0 + y;
+    return (t.first + r / a.group) * a.heads + hk * a.group + r % a.group;
+  };
+  // every split's factor 2^(m_i - m) and the sum of all, once per row
+  __shared__ float2 ml[16][kMostSplits];
+  __shared__ float2 whole[16];
+  for (int x = threadIdx.x; x < here * used; x += 256)
+    ml[x / used][x % used] = a.part_ml[x % used * rows + row(x / used)];
+  __syncthreads();
+  if (threadIdx.x < here) {
+    const int y = threadIdx.x;
+    float m = -INFINITY, l = 0.0f;
+    for (int i = 0; i < used; ++i) m = fmaxf(m, ml[y][i].x);
     const float base = m == -INFINITY ? 0.0f : m;
-    f32x4 v{};
-    float l = 0.0f;
-#pragma unroll 4
     for (int i = 0; i < used; ++i) {
-      const float2 ml = a.part_ml[i * rows + at];
-      const float f = __builtin_amdgcn_exp2f(ml.x - base);
-      l += ml.y * f;
-      v += *reinterpret_cast<const f32x4*>(a.part + (i * rows + at) * dim + d) * f;
+      const float f = __builtin_amdgcn_exp2f(ml[y][i].x - base);
+      l += ml[y][i].y * f;
+      ml[y][i].x = f;
     }
+    whole[y] = float2{m, l};
+  }
+  __syncthreads();
+  for (int x = threadIdx.x; x < here * quads; x += 256) {
+    const int y = x / quads, d = x % quads * 4;
+    const int r = t.row0 + y0 + y, tok = r / a.group, h = hk * a.group + r % a.group;
+    const int64_t at = row(y);
+    f32x4 v{};
+#pragma unroll 8
+    for (int i = 0; i < used; ++i)
+      v += *reinterpret_cast<const f32x4*>(a.part + (i * rows + at) * dim + d) * ml[y][i].x;
+    const float m = whole[y].x, l = whole[y].y;
     const float inv = 1.0f / l;
     Loose<T, 4> w;
 #pragma unroll

@@ -378,7 +378,7 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
                     pairs[4 * step + 3]};
       o[b] = mul32<T>(v, p, o[b]);
     };
-    auto no_work = [](int) {};
+    [[maybe_unused]] auto no_work = [](int) {};
     auto only = [&](auto buf) {   // values in place, since only this step reads them
       for (int x = (int)threadIdx.x * 4; x < S::VBYTES; x += 256 * kWaves) {
         uint32_t* w = reinterpret_cast<uint32_t*>(&vt(buf)[x]);
