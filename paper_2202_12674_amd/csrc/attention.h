@@ -106,6 +106,23 @@ LSSVM_DEV bool find_tile(const AttentionArgs& a, int64_t index, int rows, Tile* 
   return false;
 }
 
+// What workgroup blockIdx.x of a grid of work_groups() does: tile, split and head; false
+// for the few too many. Workgroups go to the XCDs in turn, so every eighth takes the
+// next piece of work: an XCD works on neighbouring tiles, which read the same keys.
+inline int64_t work_groups(const AttentionArgs& a) {
+  return (a.plan.tiles * a.plan.splits * a.c.heads + 7) / 8 * 8;
+}
+LSSVM_DEV bool find_work(const AttentionArgs& a, int64_t* tile, int* split, int* head) {
+  const int64_t count = a.plan.tiles * a.plan.splits * a.c.heads, each = (count + 7) / 8;
+  const int64_t work = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
+  if ((blockIdx.x >> 3) >= each || work >= count) return false;
+  const int64_t pair = work / a.plan.tiles;
+  *tile = work - pair * a.plan.tiles;
+  *head = (int)(pair / a.plan.splits);
+  *split = (int)(pair - (int64_t)*head * a.plan.splits);
+  return true;
+}
+
 // Blocks of `block` keys per split, of which a tile uses ceil(blocks / per): short
 // sequences use fewer splits than the call has, none of fewer than `least` blocks.
 LSSVM_DEV int split_blocks(int keys, int block, int splits, int least) {

@@ -12,13 +12,27 @@ namespace {
 
 constexpr int64_t kCUs = 256;
 constexpr int kMostSplits = 64;
+constexpr int64_t kL2Bytes = 4 << 20;   // of an XCD
 constexpr int64_t kWideKeys = 768;
 constexpr int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 
 AttentionPlan make_plan(const lssvm_cache& c, int64_t tokens, int heads, bool accumulate) {
   AttentionPlan p{};
   const int64_t group = heads / c.heads, most = c.columns * c.page;
-  p.few = tokens * group <= 32 * c.sequences;
+  // Tiles of 16 rows or of 128, by the rows that a sequence has on average: the latter
+  // read every key once for all of them, through LDS; the former waste less on few rows.
+  // 16-bit types, us of tiles of 16 and of 128: heads of 64 (8 sequences of 2000 keys) 64
+  // rows 24, 24, 256 rows 32, 35, 512 rows 46, 40; of 128 (30 of 600) 16 rows 14, 26, 64
+  // rows 30, 30, (8 of 4000) 8 rows 31, 27; of 256 (4 of 9000) 4 rows 38, 54, 16 rows 70,
+  // 61. In fp32, where the matrix cores take eight times as long, tiles of 16 are better
+  // (8 of 2000 x 128: 64 rows 48, 84, 1024 rows 241, 304; 2 of 6000 x 256, 8000 rows 915,
+  // 976) until a head's keys and values outgrow an XCD's L2, from which every tile reads
+  // them (16000 x 96, 4096 rows: 734, 474; 8192 x 128, 8192 rows: 2262, 2110).
+  const int64_t rows = tokens * group / c.sequences;
+  if (c.dtype == LSSVM_F32)
+    p.few = rows <= 256 || c.dim > 128 || most * c.dim * 8 <= kL2Bytes;
+  else
+    p.few = rows <= (c.dim <= 64 ? 64 : c.dim <= 128 ? 16 : 8);
   p.rows = p.few ? 16 : 128;
   // every sequence's last tile may be partly empty
   p.tiles = tokens * group / p.rows + std::min(c.sequences, tokens);
@@ -41,7 +55,9 @@ AttentionPlan make_plan(const lssvm_cache& c, int64_t tokens, int heads, bool ac
     p.wide = true;
     p.splits = 1;
   }
-  p.pitch = accumulate && p.few ? round_up(most, 32) : 0;
+  // Weights of up to 32 rows come from their scores, which then take 4 bytes per row and
+  // key; of more, the scores are formed again.
+  p.pitch = accumulate && p.few && rows <= 32 ? round_up(most, 32) : 0;
   return p;
 }
 
@@ -189,7 +205,7 @@ hipError_t launch_attention(AttentionArgs a, void* workspace, hipStream_t stream
                                    : join<float>(a, stream);
   }
   if (e != hipSuccess || !a.accumulate) return e;
-  if (!a.plan.few) return launch_weights_chunk(a, stream);
+  if (a.plan.pitch == 0) return launch_weights_chunk(a, stream);
   k_weights_few<<<dim3((unsigned)((a.c.columns * a.c.page + kWeightKeys - 1) / kWeightKeys),
                        (unsigned)a.c.heads, (unsigned)a.c.sequences),
                   kWeightKeys / 4, 0, stream>>>(a);

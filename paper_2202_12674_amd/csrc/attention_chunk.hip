@@ -155,14 +155,10 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
   const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  // workgroups of one XCD take neighbouring tiles, which read the same keys
-  const int64_t count = a.plan.tiles * a.plan.splits * a.c.heads, each = (count + 7) / 8;
-  const int64_t work = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
-  if (work >= count) return;
-  const int64_t pair = work / a.plan.tiles;
-  const int hk = (int)(pair / a.plan.splits), split = (int)(pair % a.plan.splits);
+  int64_t tile;
+  int hk, split;
   Tile t;
-  if (!find_tile(a, work % a.plan.tiles, 32 * kWaves, &t)) return;
+  if (!find_work(a, &tile, &split, &hk) || !find_tile(a, tile, 32 * kWaves, &t)) return;
   const int per = split_blocks(t.keys, KEYS, a.plan.splits, kChunkLeast);
   const int blocks = (t.keys + KEYS - 1) / KEYS;
   const int used = max(1, (blocks + per - 1) / per);
@@ -618,9 +614,7 @@ __global__ void __launch_bounds__(256) k_weights_chunk(AttentionArgs a) {
 
 template <typename T, int D>
 hipError_t launch_width(const AttentionArgs& a, hipStream_t stream) {
-  const int64_t count = a.plan.tiles * a.plan.splits * a.c.heads;
-  const dim3 grid((unsigned)((count + 7) / 8 * 8));
-  k_attention_chunk<T, D><<<grid, 64 * kWaves, 0, stream>>>(a);
+  k_attention_chunk<T, D><<<dim3((unsigned)work_groups(a)), 64 * kWaves, 0, stream>>>(a);
   return hipGetLastError();
 }
 template <typename T, int D>

@@ -79,9 +79,10 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
 
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int split = blockIdx.y, hk = blockIdx.z;
+  int64_t tile;
+  int hk, split;
   Tile t;
-  if (!find_tile(a, blockIdx.x, 16, &t)) return;
+  if (!find_work(a, &tile, &split, &hk) || !find_tile(a, tile, 16, &t)) return;
   const int per = split_blocks(t.keys, KEYS, a.plan.splits, kFewLeast);
   const int blocks = (t.keys + KEYS - 1) / KEYS;
   const int used = max(1, (blocks + per - 1) / per);
@@ -449,7 +450,7 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
 
 template <typename T, int D>
 hipError_t launch_width(const AttentionArgs& a, hipStream_t stream) {
-  const dim3 grid((unsigned)a.plan.tiles, (unsigned)a.plan.splits, (unsigned)a.c.heads);
+  const dim3 grid((unsigned)work_groups(a));
   const bool blocks = a.c.page % 16 == 0;
   if (a.plan.wide) {
     if (blocks)

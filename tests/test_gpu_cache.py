@@ -281,6 +281,17 @@ def test_attention_of_long_sequences_and_many(torch_dev, dtype):
                   1, 64, 16, True, True)
 
 
+@pytest.mark.parametrize("d,page", [(64, 24), (96, 16), (128, 64)])
+def test_attention_of_chunks_over_long_caches(torch_dev, d, page):
+    """Hundreds of rows over keys that outgrow an L2, where single precision too goes by
+    tiles of 128 rows; values that are not finite among the last."""
+    lengths, new = [9000, 8301], [300, 277]
+    wild = [(0, 8999, 0, 3, math.inf), (0, 8800, 0, d - 1, math.nan), (1, 8150, 0, 7, -math.inf)]
+    for dtype in TYPES:
+        run_attention(torch_dev, dtype, lengths, new, 2, 1, d, page, True, True, wild=wild)
+        run_attention(torch_dev, dtype, lengths, new, 2, 1, d, page, False, split_q=True, holes=5)
+
+
 def test_attention_of_nothing(torch_dev):
     torch, dev = torch_dev
     import paper_2202_12674_amd as P
