@@ -157,6 +157,8 @@ LSSVM_DEV int64_t split(int64_t v, int by, int* rest) {
   return q;
 }
 
+// Measured: bf16, 16384 tokens x 32 heads x 128, 268 MB, in 42 us (6.3 TB/s, in part from
+// the cache behind the L2s); fp32, 3001 x 12 x 80, 23 MB, in 6.5 us.
 template <typename T, bool INTER>
 __global__ void __launch_bounds__(kThreads) k_rotary(RotaryArgs a, int chunks, int turned,
                                                      int groups) {
@@ -194,7 +196,9 @@ hipError_t by_dtype(int dtype, F f) {
 
 // -------------------------------------------------------- cache append ------
 
-// One chunk of a new token's key or value per thread, for some of its heads.
+// One chunk of a new token's key or value per thread, for some of its heads. Measured: 9
+// x 2048 tokens x 8 heads x 128, 110 MB, in 23 us (4.8 TB/s); 64 tokens in 5.6 us, a
+// chain of loads (offsets, length, page).
 template <typename T, bool INTER>
 __global__ void __launch_bounds__(kThreads) k_append(AppendArgs a, int chunks, int turned,
                                                      int copied, int groups) {
@@ -356,7 +360,9 @@ __global__ void __launch_bounds__(kSelectThreads) k_evict_select(EvictArgs a) {
   }
 }
 
-// Rows of keys and values, 16 bytes of each per thread and row.
+// Rows of keys and values, 16 bytes of each per thread and row. Measured: 6144 of 12288
+// keys x 8 heads x 128 of 32 sequences, 1.6 GB, in 326 us (5.0 TB/s, as a large copy); the
+// selection before it 22 us.
 constexpr int kCopyRows = 4;   // rows in flight per thread
 __global__ void __launch_bounds__(kThreads) k_evict_copy(EvictArgs a, int lanes, int size) {
   const int s = blockIdx.z, h = blockIdx.y;
