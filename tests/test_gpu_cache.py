@@ -582,6 +582,65 @@ def test_calls_on_streams_of_their_own(torch_dev):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("new", [1, 90])
+def test_sequences_may_share_pages_and_weights_may_go_in_place(torch_dev, new):
+    """A shared prefix: the first pages of three sequences are the same; and weight_out
+    given as the cache's own weights."""
+    torch, dev = torch_dev
+    import cache_oracle as O
+    import paper_2202_12674_amd as P
+    cache, (k, v, table, lens, w) = make(torch, dev, "bf16", [300, 280, 333], 2, 64, 16, 7)
+    q = torch.randn(3 * new, 4, 64, generator=torch.Generator().manual_seed(1)).bfloat16()
+    off = offsets_of(torch, [new] * 3)
+    weight = cache.weight.clone()
+    P.attention(q.to(dev), cache, off.to(dev), accumulate=True)
+    first = cache.weight.clone()
+    cache.weight.copy_(weight)
+    P.attention(q.to(dev), cache, off.to(dev), accumulate=True, weight_out=cache.weight)
+    assert torch.equal(first.nan_to_num(-1), cache.weight.nan_to_num(-1))
+    table[1, :9] = table[2, :9] = table[0, :9]
+    cache.table.copy_(table)
+    y = P.attention(q.to(dev), cache, off.to(dev))
+    want, bound, _, _ = O.attention(q, k, v, table, lens, off, 0.125, True)
+    _check(y, want, bound)
+
+
+def test_calls_of_two_threads(torch_dev):
+    torch, dev = torch_dev
+    import threading
+    import paper_2202_12674_amd as P
+    cache, _ = make(torch, dev, "f16", [700, 320], 2, 64, 16, 3)
+    off = {n: offsets_of(torch, [n, n]).to(dev) for n in (1, 50)}
+    q = {n: torch.randn(2 * n, 8, 64, device=dev).half() for n in off}
+    want = {n: P.attention(q[n], cache, off[n]) for n in off}
+    torch.cuda.synchronize()
+    got, errors = {n: [] for n in off}, []
+
+    def work(n):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(20):
+                    got[n].append(P.attention(q[n], cache, off[n]))
+                    try:
+                        P.attention(q[n][:, :3], cache, off[n])
+                        errors.append("not refused")
+                    except P.LssvmError:
+                        pass
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:      # noqa: BLE001 - reported below
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(n,)) for n in off]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors
+    for n in off:
+        for y in got[n]:
+            assert torch.equal(y, want[n])
+
+
 def test_tensor_refusals(torch_dev):
     torch, dev = torch_dev
     import paper_2202_12674_amd as P
