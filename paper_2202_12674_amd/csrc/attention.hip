@@ -53,7 +53,7 @@ AttentionPlan make_plan(const lssvm_cache& c, int64_t tokens, int heads, bool ac
       1, std::min<int64_t>({want, (most + 127) / 128, p.few ? kMostSplits : 16}));
   // Short caches of few tiles: eight waves in place of four go over them whole, and
   // nothing is to be joined (1 x 500 keys 11 us against 14, 1000 15 against 14).
-  if (p.few && whole <= kCUs && most <= kWideKeys) {
+  if (p.few && c.dim <= 128 && whole <= kCUs && most <= kWideKeys) {
     p.wide = true;
     p.splits = 1;
   }

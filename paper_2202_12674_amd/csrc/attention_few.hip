@@ -51,9 +51,12 @@ struct Shape {
   static constexpr int KEYS = few_keys<T>;               // of a step
   static constexpr int KB = KEYS / 16;                   // ... blocks of 16
   static constexpr int KC = D / (4 * VE);                // 16-byte chunks of a key per lane
-  static constexpr int CE = D / 16 < VE ? D / 16 : VE;   // values of a chunk
+  static constexpr int CE = D % (16 * VE) == 0 ? VE      // values of a chunk
+                            : D / 16 < VE      ? D / 16
+                                               : 2;
   static constexpr int CW = CE * (int)sizeof(T) / 4;     // ... in words
   static constexpr int NC = D / (16 * CE);
+  static_assert(NC * 16 * CE == D && KC * 4 * VE == D, "whole parts and chunks");
   static constexpr int VR = 4 * KB;                      // rows of values per lane
 };
 
@@ -459,23 +462,28 @@ template <typename T, int D>
 hipError_t launch_width(const AttentionArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)work_groups(a));
   const bool blocks = a.c.page % 16 == 0;
-  if (a.plan.wide) {
-    if (blocks)
-      k_attention_few<T, D, true, 8><<<grid, 512, 0, stream>>>(a);
-    else
-      k_attention_few<T, D, false, 8><<<grid, 512, 0, stream>>>(a);
-  } else {
-    if (blocks)
-      k_attention_few<T, D, true, 4><<<grid, 256, 0, stream>>>(a);
-    else
-      k_attention_few<T, D, false, 4><<<grid, 256, 0, stream>>>(a);
+  if constexpr (D <= 128) {   // (eight waves have too few registers for more)
+    if (a.plan.wide) {
+      if (blocks)
+        k_attention_few<T, D, true, 8><<<grid, 512, 0, stream>>>(a);
+      else
+        k_attention_few<T, D, false, 8><<<grid, 512, 0, stream>>>(a);
+      return hipGetLastError();
+    }
   }
+  if (blocks)
+    k_attention_few<T, D, true, 4><<<grid, 256, 0, stream>>>(a);
+  else
+    k_attention_few<T, D, false, 4><<<grid, 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_type(const AttentionArgs& a, hipStream_t stream) {
   if (a.c.dim <= 64) return launch_width<T, 64>(a, stream);
+  // (in 16 bits narrower parts would take more loads than the padding costs)
+  if constexpr (sizeof(T) == 4)
+    if (a.c.dim <= 96) return launch_width<T, 96>(a, stream);
   if (a.c.dim <= 128) return launch_width<T, 128>(a, stream);
   return launch_width<T, 256>(a, stream);
 }
