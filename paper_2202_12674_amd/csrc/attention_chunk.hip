@@ -520,7 +520,7 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
 // weight_out = weight + the probabilities that the rows give to 64 keys, which stay in
 // registers: every wave takes every fourth 32 rows, forms the scores anew and sums
 // p = 2^(score - lse) per key; the waves' sums are joined in order. Measured: f16, 6 x
-// 700 rows x 14 heads over 3001 keys, 64 wide: 44 us (13.5 GFLOP); bound by reading the
+// 700 rows x 14 heads over 3001 keys, 64 wide: 47 us (13.5 GFLOP); bound by reading the
 // rows from L2, once for every 64 keys (32 keys: 70 us; rows not read ahead: 68).
 template <typename T, int D>
 __global__ void __launch_bounds__(256) k_weights_chunk(AttentionArgs a) {

@@ -73,7 +73,7 @@ struct Shape {
 // the pages hold whole runs of 16 keys, whose page is then looked up once.
 //
 // Measured (bf16, 128 wide, 8 heads of a group of 4): 64 rows over 16384 keys each, 3.1
-// GB, in 540 us, 5.7 TB/s (a large copy moves 5.1); with scores kept for the weights 690
+// GB, in 540 us, 5.7 TB/s (a large copy moves 5.1); with scores kept for the weights 665
 // us, for 100 MB of them: stores among the loads cost more than their bytes, however
 // they are laid out or hinted. 1 row over 1500 keys: 7 us, a chain of five dependent
 // loads (offsets, page, keys, values, join) on 8 x 12 workgroups. A workgroup alone on
