@@ -605,6 +605,36 @@ def test_sequences_may_share_pages_and_weights_may_go_in_place(torch_dev, new):
     _check(y, want, bound)
 
 
+@pytest.mark.parametrize("page", [64, 21])
+@pytest.mark.parametrize("new", [1, 90])
+def test_pages_beyond_32_bit_offsets(torch_dev, new, page):
+    """The same cache in a small pool and at the end of one of 5 GiB: equal in every bit."""
+    torch, dev = torch_dev
+    import paper_2202_12674_amd as P
+    heads, d = 2, 128
+    small, _ = make(torch, dev, "bf16", [500, 300], heads, d, page, 7)
+    pages = 5 * 2 ** 30 // (heads * page * d * 2)
+    base = pages - small.pages
+    k, v = (torch.empty(pages, heads, page, d, dtype=torch.bfloat16, device=dev) for _ in "kv")
+    w = torch.empty(pages, heads, page, device=dev)
+    k[base:], v[base:], w[base:] = small.k, small.v, small.weight
+    table = torch.where(small.table >= 0, small.table + base, small.table)
+    large = P.PagedCache(k, v, table, small.lengths, w)
+    q = torch.randn(2 * new, 8, d, device=dev).bfloat16()
+    nk, nv = (torch.randn(2 * new, heads, d, device=dev).bfloat16() for _ in "kv")
+    off, at = offsets_of(torch, [new, new]).to(dev), torch.arange(2 * new, device=dev)
+    f, _ = P.rotary_frequencies(d, device=dev)
+    out = []
+    for c in (small, large):
+        P.cache_append(c, nk, nv, off, at, f)
+        out.append(P.attention(q, c, off, accumulate=True))
+    assert torch.equal(out[0], out[1])
+    for a, b in ((k, small.k), (v, small.v), (w, small.weight)):
+        assert torch.equal(a[base:].nan_to_num(9.0), b.nan_to_num(9.0))
+    del k, v, w, large
+    torch.cuda.empty_cache()
+
+
 def test_calls_of_two_threads(torch_dev):
     torch, dev = torch_dev
     import threading
