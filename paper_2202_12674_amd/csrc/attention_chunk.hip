@@ -129,7 +129,8 @@ LSSVM_DEV int column_at(int d, int keys8) { return d * 128 + 16 * (keys8 ^ ((d ^
 // there once, 4 keys x 8 values per thread, so that a lane reads 8 keys of its column
 // in one piece; fp32 ones are read singly and stay in rows.
 // 16-bit types: p is rounded to the stored type for the product, half a step of it,
-// as the values themselves were; its sum is taken before that.
+// as the values themselves were; its sum is taken before that. fp16 has too short a
+// range for that: small ones are multiplied apart (attention.h).
 //
 // Measured: bf16, 4 x 2048 rows x 32 heads over 16384 keys, 128 wide: 1.69 ms, 780
 // TFLOP/s (a large library product reaches 1107). The matrix cores are busy for 34% of
@@ -318,8 +319,10 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
     };
     // masks the scores, brings the maximum and what hangs on it up to date. The maximum
     // may stay up to 2^8 behind: p is then that much larger than 1.
+    float low;   // fp16: the least score that is seen
     auto settle = [&](int block) {
       const int j0 = block * KEYS;
+      low = INFINITY;
       const uint64_t ok = there[(block - block0) & 3];
       const uint64_t ok_h = ok >> (4 * h);   // of key k + 4 h
       const int left = lim - j0 - 4 * h;
@@ -331,12 +334,16 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
             const int k = 32 * b + result_row(i, 0);
             const bool sees = k < left && (ok_h >> k & 1);
             if (counts) s[b][i] = 0.0f;   // p = 1
+            if constexpr (kShort<T>) low = sees ? fminf(low, s[b][i]) : low;
             if (!sees) s[b][i] = -INFINITY;
           }
           look_at(b);
         }
       } else {
         look_at(NB - 1);
+        if constexpr (kShort<T>)
+#pragma unroll
+          for (int i = 0; i < 16 * NB; ++i) low = fminf(low, s[i / 16][i % 16]);
       }
       const float high =
           max_across_32(fmaxf(fmaxf(highs[0], highs[1]), fmaxf(highs[2], highs[3])));
@@ -352,7 +359,7 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
           pin(o[b]);
         }
       }
-      base = counts || top == -INFINITY ? 0.0f : -top * scale2;
+      base = counts || top == -INFINITY ? 0.0f : chunk_lift<T> - top * scale2;
     };
     auto power = [&](int i) {   // p of score i
       return __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 16][i % 16], scale2, base));
@@ -383,7 +390,44 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
                     pairs[4 * step + 3]};
       o[b] = mul32<T>(v, p, o[b]);
     };
-    [[maybe_unused]] auto no_work = [](int) {};
+    // fp16: the step's probabilities below 2^kChunkFaint, and none of them after that
+    auto add_faint = [&](auto buf) {
+      if constexpr (kShort<T>) {
+        typedef T t2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int b = 0; b < DB; ++b) o[b] *= __builtin_ldexpf(1.0f, kChunkFar);
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          uint32_t far[8];
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            t2 w;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float power = __builtin_fmaf(s[n][2 * x + e], scale2, base);
+              const bool faint = power < (float)kChunkFaint;
+              const float p = faint ? __builtin_amdgcn_exp2f(power + kChunkFar) : 0.0f;
+              l += p * __builtin_ldexpf(1.0f, -kChunkFar);
+              w[e] = (T)p;
+              if (faint) s[n][2 * x + e] = -INFINITY;
+            }
+            far[x] = __builtin_bit_cast(uint32_t, w);
+          }
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int b = 0; b < DB; ++b)
+              o[b] = mul32<T>(read_column(buf, (2 * n + x) * DB + b),
+                              u32x4{far[4 * x], far[4 * x + 1], far[4 * x + 2], far[4 * x + 3]},
+                              o[b]);
+        }
+#pragma unroll
+        for (int b = 0; b < DB; ++b) {
+          o[b] *= __builtin_ldexpf(1.0f, -kChunkFar);
+          pin(o[b]);
+        }
+      }
+    };
     auto only = [&](auto buf) {   // values in place, since only this step reads them
       for (int x = (int)threadIdx.x * 4; x < S::VBYTES; x += 256 * kWaves) {
         uint32_t* w = reinterpret_cast<uint32_t*>(&vt(buf)[x]);
@@ -420,6 +464,9 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
                              if (NB == 2 && n == KC) look_at(0);
                            });
         settle(block);
+        if constexpr (kShort<T>)
+          if (!counts && __any(__builtin_fmaf(low, scale2, base) < (float)kChunkFaint))
+            add_faint(buf);
         if constexpr (HALF) {
           // the probabilities of 16 keys while those of the 16 before are multiplied
           make_pairs(0, 4);
@@ -492,9 +539,10 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
       }
     if (kind == Kind::finite && h == 0) {
       if (used > 1)
-        a.part_ml[split * rows + at] = float2{top * scale2, sum};
+        a.part_ml[split * rows + at] = float2{top * scale2 - chunk_lift<T>, sum};
       else if (a.lse)
-        a.lse[at] = sum == 0.0f ? INFINITY : top * scale2 + __builtin_amdgcn_logf(sum);
+        a.lse[at] = sum == 0.0f ? INFINITY
+                                : top * scale2 - chunk_lift<T> + __builtin_amdgcn_logf(sum);
     }
   };
 

@@ -235,6 +235,7 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
   // O^T += V^T p for the step's values: `hi` and `lo` are the 16-bit parts of p, in fp32
   // p itself. WILD: values that are not finite are left out of that, and enter as
   // codes times whether the row sees the key, `see` (as a vector of T, or fp32).
+  uint32_t picks[2] = {0x05040100u, 0x07060302u};   // the even, the odd values of two words
   auto add_values = [&](auto with_wild, u32x4 hi, u32x4 lo, u32x4 see, f32x4 p) {
     constexpr bool WILD = decltype(with_wild)::value;
 #pragma unroll
@@ -244,10 +245,10 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
         f32x4& acc = o[part * CE + e];
         u32x4 v;
         if constexpr (HALF) {
-          const uint32_t pick = e & 1 ? 0x07060302u : 0x05040100u;
 #pragma unroll
           for (int u = 0; u < 4; ++u)
-            v[u] = __builtin_amdgcn_perm(vf[2 * u + 1][part][e / 2], vf[2 * u][part][e / 2], pick);
+            v[u] = __builtin_amdgcn_perm(vf[2 * u + 1][part][e / 2], vf[2 * u][part][e / 2],
+                                         picks[e & 1]);
         } else {
 #pragma unroll
           for (int i = 0; i < 4; ++i) v[i] = vf[i][part][e];
@@ -351,7 +352,7 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
 #pragma unroll
         for (int e = 0; e < NC * CE; ++e) o[e] *= old;
       }
-      const float base = top == -INFINITY ? 0.0f : top;
+      const float base = top == -INFINITY ? 0.0f : top - few_lift<T>;
       f32x4 p[KB];
 #pragma unroll
       for (int b = 0; b < KB; ++b)
@@ -360,35 +361,59 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
           p[b][i] = __builtin_amdgcn_exp2f(s[b][i] - base);
           l += p[b][i];
         }
-      u32x4 hi{}, lo{};
-      if constexpr (HALF) {
-        typedef T t8 __attribute__((ext_vector_type(8)));
-        t8 h, d;
+      // fp16: the least p that is not 0, as bits less one, tells whether any is faint
+      const float faint = __builtin_ldexpf(1.0f, kFewFaint);
+      bool far = false;
+      if constexpr (kShort<T>) {
+        uint32_t least = ~0u;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          h[i] = (T)p[i / 4][i % 4];
-          d[i] = (T)(p[i / 4][i % 4] - (float)h[i]);
-        }
-        hi = __builtin_bit_cast(u32x4, h);
-        lo = __builtin_bit_cast(u32x4, d);
+        for (int i = 0; i < 8; ++i) least = min(least, __float_as_uint(p[i / 4][i % 4]) - 1);
+        far = __any(least < __float_as_uint(faint) - 1);
       }
-
-      if constexpr (decltype(with_wild)::value) {
-        u32x4 see;
+      const bool parted = far;   // the faint ones go first, then the others
+#pragma unroll 1
+      do {
+        if constexpr (kShort<T>)   // (or all of the transposed values are kept over the loop)
+          asm volatile("" : "+s"(picks[0]), "+s"(picks[1]));
+        u32x4 hi{}, lo{}, see{};
         if constexpr (HALF) {
           typedef T t8 __attribute__((ext_vector_type(8)));
-          t8 h;
+          t8 h, d;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) h[i] = s[i / 4][i % 4] == -INFINITY ? (T)0.0f : (T)1.0f;
-          see = __builtin_bit_cast(u32x4, h);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) see[i] = s[0][i] == -INFINITY ? 0 : __float_as_uint(1.0f);
+          for (int i = 0; i < 8; ++i) {
+            float x = p[i / 4][i % 4];
+            if (kShort<T> && parted)
+              x = (x < faint) != far ? 0.0f
+                  : far              ? __builtin_amdgcn_exp2f(s[i / 4][i % 4] - base + kFewFar)
+                                     : x;
+            h[i] = (T)x;
+            d[i] = (T)(x - (float)h[i]);
+          }
+          hi = __builtin_bit_cast(u32x4, h);
+          lo = __builtin_bit_cast(u32x4, d);
         }
+        if constexpr (decltype(with_wild)::value) {
+          if constexpr (HALF) {
+            typedef T t8 __attribute__((ext_vector_type(8)));
+            t8 h;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              h[i] = far || s[i / 4][i % 4] == -INFINITY ? (T)0.0f : (T)1.0f;
+            see = __builtin_bit_cast(u32x4, h);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) see[i] = s[0][i] == -INFINITY ? 0 : __float_as_uint(1.0f);
+          }
+        }
+        if (far)
+#pragma unroll
+          for (int e = 0; e < NC * CE; ++e) o[e] *= __builtin_ldexpf(1.0f, kFewFar);
         add_values(with_wild, hi, lo, see, p[0]);
-      } else {
-        add_values(with_wild, hi, lo, u32x4{}, p[0]);
-      }
+        if (!far) break;
+#pragma unroll
+        for (int e = 0; e < NC * CE; ++e) o[e] *= __builtin_ldexpf(1.0f, -kFewFar);
+        far = false;
+      } while (kShort<T>);
       load_values(next);
       now = next;
       next = after;
@@ -404,6 +429,7 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
 #pragma unroll
     for (int i = 0; i < 4; ++i) finite &= __builtin_isfinite(o[e][i]);
   if (__any(!finite)) sweep(std::true_type{});
+  top -= few_lift<T>;   // as the sums are lifted
 
   // join the waves' sums
   l += __shfl_xor(l, 16);
