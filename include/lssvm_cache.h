@@ -88,7 +88,8 @@ int lssvm_rotary_frequencies(int64_t pairs, double base, int32_t scaling, double
  * x, out       device, tokens x heads x dim values of dtype; strides of token and
  *              head in elements (host, 2 each), the dim values contiguous. out may be
  *              x itself with the same strides, else they must not overlap.
- * positions    device, tokens integers of position_bytes (4 or 8) bytes; any sign.
+ * positions    device, tokens integers of position_bytes (4 or 8) bytes; any sign and
+ *              size (from 2^53 on as the nearest double). An infinite angle gives NaN.
  * freqs        device, pairs doubles, 0 <= 2 * pairs <= dim. The first 2 * pairs values
  *              of a head are turned; the others are copied.
  * interleaved  nonzero: pair i is (2i, 2i + 1), else (i, i + pairs).

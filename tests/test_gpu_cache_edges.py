@@ -81,3 +81,36 @@ def test_weights_of_all_sizes_in_half_precision(torch_dev, new, least):
     gaps[0] = 0.0
     v = (2e4 + 4e4 * torch.rand(3000, 64, generator=g)) * (gaps >= least)[:, None]
     _faint(torch, dev, gaps.tolist(), v, new, 16)
+
+
+# ----------------------------------------------------------- wide angles ----
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_rotary_of_positions_as_large_as_their_type(torch_dev, dtype, interleaved):
+    """The angle is position x frequency in fp64, however large; an infinite one is NaN."""
+    torch, dev = torch_dev
+    import cache_oracle as O
+    import paper_2202_12674_amd as P
+    g = torch.Generator().manual_seed(3)
+    near = [s * 2 ** e + o for e in (30, 40, 44, 45, 46, 49, 52, 53, 55, 58, 62) for s in (1, -1)
+            for o in (-1, 0, 1)]
+    pos = torch.tensor(near + [2 ** 63 - 1, -2 ** 63, 0], dtype=torch.int64)
+    f = torch.tensor([1.0, 0.7390851332151607, 1e-3, 1e-9, 3.0, 1e5, 1e30, 1e300],
+                     dtype=torch.float64)
+    x = torch.randn(len(pos), 2, 21, generator=g)
+    x = x.half() if dtype == "f16" else x
+    y = P.rotary(x.to(dev), pos.to(dev), f.to(dev), interleaved=interleaved).double().cpu()
+    for t in range(len(pos)):
+        angles = [float(pos[t]) * a for a in f.tolist()]
+        for i, a in enumerate(angles):
+            m, n = (2 * i, 2 * i + 1) if interleaved else (i, i + len(angles))
+            x0, x1 = x[t, :, m].double(), x[t, :, n].double()
+            if math.isinf(a):
+                assert bool(y[t, :, [m, n]].isnan().all())
+                continue
+            c, s = math.cos(a), math.sin(a)
+            for at, want in ((m, x0 * c - x1 * s), (n, x1 * c + x0 * s)):
+                bound = O.rotary_bound(want, x0.abs() + x1.abs(), x.dtype)
+                assert bool(((y[t, :, at] - want).abs() <= bound).all()), (int(pos[t]), a)
+    assert torch.equal(y[..., 16:], x[..., 16:].double())
