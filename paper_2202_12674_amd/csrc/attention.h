@@ -66,6 +66,17 @@ constexpr int kFewFaint = -10, kFewFar = 25;
 template <typename T>
 constexpr int chunk_lift = kShort<T> ? 7 : 0;
 constexpr int kChunkFaint = -14, kChunkFar = 29;
+
+// Sums of values up to the largest of their type overflow where their mean does not. Sums
+// of up to kSafeSum are joined as they are (512 of them are finite); where one is larger
+// or not finite, the keys are gone over again, with values that are not finite apart and
+// probabilities so much smaller that sums over `keys` of them stay in range. (fp16 values
+// cannot get there.)
+constexpr float kSafeSum = 5.192296858534828e33f;   // 2^112
+template <typename T>
+__device__ inline float lowered(int lift, int most, int keys) {
+  return kShort<T> ? lift : -(float)(most + 33 - __clz(keys));   // p <= 2^most
+}
 // ------------------------------------------------------------- device -------
 
 struct Tile {

@@ -297,9 +297,11 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
   // One pass over the keys. Pass 0 is the only one unless values are not finite; the
   // others count only the values of one kind (below).
   f32x16 s[NB];
-  float base;
+  float base, lift;
+  bool taken = false;   // whether the pass without values that are not finite met any
   auto sweep = [&](int pass) {
     const Kind kind = (Kind)(pass - 1);
+    lift = pass == 0 ? chunk_lift<T> : lowered<T>(chunk_lift<T>, 8, t.keys);
     const bool counts = pass > 1;
     // scores: products of keys and queries, one block of 32 keys after the other
     auto read_key = [&](auto buf, int n) {
@@ -359,7 +361,7 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
           pin(o[b]);
         }
       }
-      base = counts || top == -INFINITY ? 0.0f : chunk_lift<T> - top * scale2;
+      base = counts || top == -INFINITY ? 0.0f : lift - top * scale2;
     };
     auto power = [&](int i) {   // p of score i
       return __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 16][i % 16], scale2, base));
@@ -431,7 +433,9 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
     auto only = [&](auto buf) {   // values in place, since only this step reads them
       for (int x = (int)threadIdx.x * 4; x < S::VBYTES; x += 256 * kWaves) {
         uint32_t* w = reinterpret_cast<uint32_t*>(&vt(buf)[x]);
-        *w = only_kind<T>(*w, kind);
+        const uint32_t was = *w, is = only_kind<T>(was, kind);
+        taken |= kind == Kind::finite && is != was;
+        *w = is;
       }
       __syncthreads();
     };
@@ -539,16 +543,17 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
       }
     if (kind == Kind::finite && h == 0) {
       if (used > 1)
-        a.part_ml[split * rows + at] = float2{top * scale2 - chunk_lift<T>, sum};
+        a.part_ml[split * rows + at] = float2{top * scale2 - lift, sum};
       else if (a.lse)
         a.lse[at] = sum == 0.0f ? INFINITY
-                                : top * scale2 - chunk_lift<T> + __builtin_amdgcn_logf(sum);
+                                : top * scale2 - lift + __builtin_amdgcn_logf(sum);
     }
   };
 
   // A value that is not finite makes its product with any probability so, zeros of rows
   // that do not see it among them. Then the keys are gone over again without such
-  // values, and once more for each kind of them.
+  // values, and once more for each kind of them if there were any (there are none where
+  // sums of finite ones came near their end).
 #pragma unroll 1
   for (int pass = 0; pass < 5; ++pass) {
     sweep(pass);
@@ -557,11 +562,11 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
 #pragma unroll
         for (int b = 0; b < DB; ++b)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) wild |= !__builtin_isfinite(o[b][i]);
+          for (int i = 0; i < 16; ++i) wild |= !(fabsf(o[b][i]) < kSafeSum);
       if (__syncthreads_or(wild)) continue;
     }
     write(pass == 0 ? Kind::finite : (Kind)(pass - 1));
-    if (pass == 0) break;
+    if (pass == 0 || (pass == 1 && !__syncthreads_or(taken))) break;
   }
 }
 

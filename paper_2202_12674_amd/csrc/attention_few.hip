@@ -231,6 +231,7 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
 
   f32x4 o[NC * CE];
   float top, l;
+  const float lift_again = lowered<T>(few_lift<T>, 0, t.keys);
 
   // O^T += V^T p for the step's values: `hi` and `lo` are the 16-bit parts of p, in fp32
   // p itself. WILD: values that are not finite are left out of that, and enter as
@@ -284,6 +285,7 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
   };
 
   auto sweep = [&](auto with_wild) {
+    const float lift = decltype(with_wild)::value ? lift_again : few_lift<T>;
 #pragma unroll
     for (int e = 0; e < NC * CE; ++e) o[e] = f32x4{};
     top = -INFINITY, l = 0.0f;
@@ -352,7 +354,7 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
 #pragma unroll
         for (int e = 0; e < NC * CE; ++e) o[e] *= old;
       }
-      const float base = top == -INFINITY ? 0.0f : top - few_lift<T>;
+      const float base = top == -INFINITY ? 0.0f : top - lift;
       f32x4 p[KB];
 #pragma unroll
       for (int b = 0; b < KB; ++b)
@@ -418,18 +420,18 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
       now = next;
       next = after;
     }
+    top -= lift;   // as the sums are lifted
   };
   // A value that is not finite makes its product with any probability so, zeros of rows
   // that do not see it among them: then the wave's keys are gone over once more, with
-  // such values apart.
+  // such values apart (and where sums of finite ones come near their end).
   sweep(std::false_type{});
-  bool finite = true;
+  bool safe = true;
 #pragma unroll
   for (int e = 0; e < NC * CE; ++e)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) finite &= __builtin_isfinite(o[e][i]);
-  if (__any(!finite)) sweep(std::true_type{});
-  top -= few_lift<T>;   // as the sums are lifted
+    for (int i = 0; i < 4; ++i) safe &= fabsf(o[e][i]) < kSafeSum;
+  if (__any(!safe)) sweep(std::true_type{});
 
   // join the waves' sums
   l += __shfl_xor(l, 16);

@@ -114,3 +114,33 @@ def test_rotary_of_positions_as_large_as_their_type(torch_dev, dtype, interleave
                 bound = O.rotary_bound(want, x0.abs() + x1.abs(), x.dtype)
                 assert bool(((y[t, :, at] - want).abs() <= bound).all()), (int(pos[t]), a)
     assert torch.equal(y[..., 16:], x[..., 16:].double())
+
+
+# ------------------------------------------------------------ wide values ---
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new,L,d,page", [(n, *c) for n in (1, 200) for c in (
+    (300, 64, 16), (5000, 128, 21), (2000, 256, 32))] + [(300, 5000, 128, 16)])
+def test_values_near_the_largest(torch_dev, dtype, new, L, d, page):
+    """A mean of finite values is finite, though their sum is not; an infinity among them
+    reaches the rows that see it."""
+    torch, dev = torch_dev
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator().manual_seed(4)
+    k, q = torch.randn(L, d, generator=g).to(dt), torch.randn(new, 1, d, generator=g)
+    q = (q / math.sqrt(d)).to(dt)
+    v = (3e38 * (0.5 + 0.5 * torch.rand(L, d, generator=g))).to(dt)
+    v[:, 1] = torch.randn(L, generator=g).abs().to(dt)      # an ordinary column among them
+    v[L - 1 - new // 2, 5] = math.inf
+    y = attend(torch, dev, q, k, v, page, causal=True)[0][:, 0].double()
+    z = q[:, 0].double() @ k.double().T
+    z[torch.arange(L)[None, :] > L - new + torch.arange(new)[:, None]] = -math.inf
+    p = torch.softmax(z, 1)
+    want = p @ torch.where(v.isinf(), 0.0, v.double())
+    want[p[:, L - 1 - new // 2] > 0, 5] = math.inf
+    reach = float((q.double().abs()[:, 0] @ k.double().abs().T).max())
+    rel = 2 * U * (2 * (d + 4) * reach + 2 * L + 16) + \
+        (2 * 2.0 ** -9 * 2 if dtype == "bf16" else 2 * U)
+    fine = want.isfinite()
+    assert torch.equal(fine, y.isfinite()) and torch.equal(y[~fine], want[~fine])
+    assert bool(((y - want).abs() <= rel * want)[fine].all())
