@@ -37,7 +37,7 @@ struct AttentionArgs {
   // workspace
   float* lse;          // per row: log2 of the sum of exponentials (with weights)
   float* part;         // splits x rows x dim: sums of one split, and
-  float2* part_ml;     // ... its maximum and sum of exponentials
+  float2* part_ml;     // ... its maximum and sum of exponentials (-1 where sees_any)
   float* scores;       // rows x pitch
 };
 
@@ -90,6 +90,15 @@ struct Tile {
 LSSVM_DEV int seen_keys(const AttentionArgs& a, const Tile& t, int r) {
   const int k = a.causal ? t.length - t.n + r / a.group + 1 : t.length;
   return k > 0 ? k : 0;
+}
+
+// Whether row r sees a key of [from, to) that is there. Asked of rows without a sum: all
+// that they see then has scores of minus infinity, and no softmax.
+LSSVM_DEV bool sees_any(const AttentionArgs& a, const Tile& t, int r, int from, int to) {
+  to = min(to, seen_keys(a, t, r));
+  for (int j = from, slot; j < to; j += (int)a.c.page - slot)
+    if (cache_page(a.c, t.s, j, &slot) >= 0) return true;
+  return false;
 }
 
 LSSVM_DEV void sequence_rows(const AttentionArgs& a, int s, int64_t* first, int* n) {
@@ -191,7 +200,8 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // A word of one or two values of T with zeros where they are not finite, and a word of
 // codes for those: small numbers of which sums of up to 63 tell how many infinities of
-// either sign and NaNs there were.
+// either sign and NaNs there were. Times kCodeNan they count as NaNs: what is not finite
+// gives that under a weight of exactly 0.
 constexpr float kCodePlus = 1.0f, kCodeMinus = 64.0f, kCodeNan = 4096.0f;
 template <typename T>
 LSSVM_DEV u32x2 take_wild(uint32_t word) {

@@ -113,12 +113,14 @@ __global__ void __launch_bounds__(256) k_attention_join(AttentionArgs a, int blo
     float m = -INFINITY, l = 0.0f;
     for (int i = 0; i < used; ++i) m = fmaxf(m, ml[y][i].x);
     const float base = m == -INFINITY ? 0.0f : m;
+    bool sees = false;
     for (int i = 0; i < used; ++i) {
       const float f = __builtin_amdgcn_exp2f(ml[y][i].x - base);
       l += ml[y][i].y * f;
+      sees |= ml[y][i].y < 0.0f;
       ml[y][i].x = f;
     }
-    whole[y] = float2{m, l};
+    whole[y] = float2{m, l == 0.0f && sees ? __builtin_nanf("") : l};
   }
   __syncthreads();
   for (int x = threadIdx.x; x < here * quads; x += 256) {

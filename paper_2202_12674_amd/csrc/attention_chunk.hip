@@ -65,8 +65,8 @@ LSSVM_DEV void read_ahead(R read, U use, W side) {
 }
 
 // Kinds of values, and the values of a word that are of one: finite ones as they are,
-// others as 1.
-enum class Kind { finite, plus, minus, nan };
+// others as 1. `lost` are all that are not finite, under scores of minus infinity.
+enum class Kind { finite, plus, minus, nan, lost };
 LSSVM_DEV float wild_value(Kind kind) {
   return kind == Kind::plus ? INFINITY : kind == Kind::minus ? -INFINITY : __builtin_nanf("");
 }
@@ -81,7 +81,7 @@ LSSVM_DEV uint32_t only_kind(uint32_t word, Kind kind) {
                    : v != v              ? Kind::nan
                    : v > 0               ? Kind::plus
                                          : Kind::minus;
-    if (k != kind)
+    if (k != kind && (kind != Kind::lost || k == Kind::finite))
       x[i] = (T)0.0f;
     else if (k != Kind::finite)
       x[i] = (T)1.0f;
@@ -335,7 +335,8 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
           for (int i = 0; i < 16; ++i) {
             const int k = 32 * b + result_row(i, 0);
             const bool sees = k < left && (ok_h >> k & 1);
-            if (counts) s[b][i] = 0.0f;   // p = 1
+            if (counts)   // p = 1
+              s[b][i] = kind != Kind::lost || s[b][i] == -INFINITY ? 0.0f : -INFINITY;
             if constexpr (kShort<T>) low = sees ? fminf(low, s[b][i]) : low;
             if (!sees) s[b][i] = -INFINITY;
           }
@@ -509,8 +510,10 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
   const int64_t rows = a.tokens * a.heads;
   auto write = [&](Kind kind) {
     const int y = wave * 32 + c;
-    const float sum = l + __shfl_xor(l, 32);
+    float sum = l + __shfl_xor(l, 32);
     if (y >= t.rows) return;
+    if (sum == 0.0f && sees_any(a, t, t.row0 + y, block0 * KEYS, block1 * KEYS))
+      sum = used == 1 ? __builtin_nanf("") : -1.0f;
     const int r = t.row0 + y, tok = r / a.group, head = hk * a.group + r % a.group;
     const int64_t at = (t.first + tok) * a.heads + head;
     T* out = static_cast<T*>(a.out) + (t.first + tok) * a.os.outer + head * a.os.head;
@@ -555,7 +558,7 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
   // values, and once more for each kind of them if there were any (there are none where
   // sums of finite ones came near their end).
 #pragma unroll 1
-  for (int pass = 0; pass < 5; ++pass) {
+  for (int pass = 0; pass < 6; ++pass) {
     sweep(pass);
     if (pass == 0) {
       int wild = 0;

@@ -78,8 +78,12 @@ struct Shape {
 // they are laid out or hinted. 1 row over 1500 keys: 7 us, a chain of five dependent
 // loads (offsets, page, keys, values, join) on 8 x 12 workgroups. A workgroup alone on
 // its CU reads 60 GB/s, which is why short caches too are split.
+//
+// (Two waves a SIMD are asked for where they fit, since the second sweep, which hardly a
+// call makes, else takes registers enough to leave one: 64 single tokens over 3001 keys
+// in fp16 157 us in place of 145.)
 template <typename T, int D, bool BLOCKS, int kWaves>
-__global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) {
+__global__ void __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) k_attention_few(AttentionArgs a) {
   using S = Shape<T, D>;
   constexpr int VE = S::VE, KB = S::KB, KEYS = S::KEYS, KC = S::KC, CE = S::CE, CW = S::CW,
                 NC = S::NC, VR = S::VR;
@@ -235,7 +239,8 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
 
   // O^T += V^T p for the step's values: `hi` and `lo` are the 16-bit parts of p, in fp32
   // p itself. WILD: values that are not finite are left out of that, and enter as
-  // codes times whether the row sees the key, `see` (as a vector of T, or fp32).
+  // codes times whether the row sees the key, `see` (as a vector of T, or fp32), where a
+  // key of score minus infinity makes any of them a NaN.
   uint32_t picks[2] = {0x05040100u, 0x07060302u};   // the even, the odd values of two words
   auto add_values = [&](auto with_wild, u32x4 hi, u32x4 lo, u32x4 see, f32x4 p) {
     constexpr bool WILD = decltype(with_wild)::value;
@@ -395,16 +400,19 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
           lo = __builtin_bit_cast(u32x4, d);
         }
         if constexpr (decltype(with_wild)::value) {
+          auto seen = [&](int b, int i) {
+            const bool sees = !masked || (16 * b + i < lim - j0 - 4 * g && (there >> (4 * b + i) & 1));
+            return far || !sees ? 0.0f : s[b][i] == -INFINITY ? kCodeNan : 1.0f;
+          };
           if constexpr (HALF) {
             typedef T t8 __attribute__((ext_vector_type(8)));
             t8 h;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              h[i] = far || s[i / 4][i % 4] == -INFINITY ? (T)0.0f : (T)1.0f;
+            for (int i = 0; i < 8; ++i) h[i] = (T)seen(i / 4, i % 4);
             see = __builtin_bit_cast(u32x4, h);
           } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) see[i] = s[0][i] == -INFINITY ? 0 : __float_as_uint(1.0f);
+            for (int i = 0; i < 4; ++i) see[i] = __float_as_uint(seen(0, i));
           }
         }
         if (far)
@@ -469,6 +477,8 @@ __global__ void __launch_bounds__(64 * kWaves) k_attention_few(AttentionArgs a) 
 #pragma unroll
     for (int w = 0; w < kWaves; ++w)
       total += sum_l[w][y] * __builtin_amdgcn_exp2f(sum_m[w][y] - (high == -INFINITY ? 0.0f : high));
+    if (total == 0.0f && sees_any(a, t, t.row0 + y, block0 * KEYS, block1 * KEYS))
+      total = last ? __builtin_nanf("") : -1.0f;
     const int tok = (t.row0 + y) / a.group, h = hk * a.group + (t.row0 + y) % a.group;
     const int64_t at = (t.first + tok) * a.heads + h;
     if (last) {

@@ -144,3 +144,46 @@ def test_values_near_the_largest(torch_dev, dtype, new, L, d, page):
     fine = want.isfinite()
     assert torch.equal(fine, y.isfinite()) and torch.equal(y[~fine], want[~fine])
     assert bool(((y - want).abs() <= rel * want)[fine].all())
+
+
+# -------------------------------------------------- scores that are infinite ---
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("new,L,page", [(1, 400, 16), (1, 1500, 21), (150, 400, 16), (150, 1500, 21),
+                                        (300, 9000, 32)])
+def test_scores_of_minus_infinity(torch_dev, dtype, new, L, page):
+    """Such a key weighs exactly nothing: finite values under it are left out, one that is
+    not finite gives NaN; and a row of no other keys has no softmax."""
+    torch, dev = torch_dev
+    dt = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}[dtype]
+    g = torch.Generator().manual_seed(5)
+    d = 64
+    k, v = torch.randn(L, d, generator=g).to(dt), torch.randn(L, d, generator=g).to(dt)
+    q = torch.zeros(new, 1, d, dtype=dt)
+    q[..., 0] = 1.0
+    lost = [3, 77, L - new // 2 - 1, L - 1]
+    k[lost, 0] = -math.inf
+    v[3, 5], v[77, 6], v[L - new // 2 - 1, 7] = math.inf, math.nan, -math.inf
+    v[8, 9], v[9, 10] = math.inf, math.nan                   # under finite scores
+    y = attend(torch, dev, q, k, v, page, causal=True)[0][:, 0].double()
+    z = (q[:, 0].double() @ torch.where(k.isinf(), 0.0, k.double()).T)
+    z[:, lost] = -math.inf
+    seen = torch.arange(L)[None, :] <= L - new + torch.arange(new)[:, None]
+    p = torch.softmax(torch.where(seen, z, -math.inf), 1)
+    want, size = (p @ torch.where(v.isfinite(), x, 0.0) for x in (v.double(), v.double().abs()))
+    want[:, [5, 6, 10]], want[:, 9] = math.nan, math.inf
+    want[seen[:, L - new // 2 - 1], 7] = math.nan
+    half = torch.finfo(dt).eps / 2
+    bound = half * want.abs() + (half * (dtype != "f32") + U * (4 * L + 4 * d * 8)) * size + 1e-7
+    fine = want.isfinite()
+    assert torch.equal(want.isnan(), y.isnan()) and torch.equal(want.isinf(), y.isinf())
+    assert bool(((y - want).abs() <= bound)[fine].all())
+
+    k[:, 0] = -math.inf
+    y, w = attend(torch, dev, q, k, v, page, causal=True, accumulate=True)
+    assert bool(y.isnan().all()) and bool(w.isnan().all())
+    k[L - new, 0] = 2.0                                      # one key that is seen by all
+    y = attend(torch, dev, q, k, v, page, causal=True)[0][:, 0]
+    others = [x for x in range(d) if x not in (5, 6, 7, 9, 10)]
+    only = v[L - new, others].double()
+    assert bool(((y[:, others].double() - only).abs() <= 8 * U * only.abs()).all())
