@@ -9,6 +9,9 @@ namespace lssvm {
 namespace {
 
 constexpr int kThreads = 256;
+// Blocks of one launch, whose grid has less than 2^32 threads along a side; what needs
+// more goes in pieces.
+constexpr int64_t kMostBlocks = 1 << 23;
 
 // ------------------------------------------------------ rotary positions ----
 
@@ -375,14 +378,15 @@ __global__ void __launch_bounds__(kSelectThreads) k_evict_select(EvictArgs a) {
 // keys x 8 heads x 128 of 32 sequences, 1.6 GB, in 326 us (5.0 TB/s, as a large copy); the
 // selection before it 22 us.
 constexpr int kCopyRows = 4;   // rows in flight per thread
-__global__ void __launch_bounds__(kThreads) k_evict_copy(EvictArgs a, int lanes, int size) {
+__global__ void __launch_bounds__(kThreads) k_evict_copy(EvictArgs a, int from_row, int lanes,
+                                                         int size) {
   const int s = blockIdx.z, h = blockIdx.y;
   const int n = min(cache_length(a.from, s), a.budget);
   const int rows = kThreads / lanes;   // rows that a block moves at once
   const int row = threadIdx.x / lanes, at = threadIdx.x % lanes;
   if (row >= rows) return;
   const int32_t* kept = a.kept + ((int64_t)s * a.from.heads + h) * a.budget;
-  const int first = blockIdx.x * rows * kCopyRows + row;
+  const int first = from_row + blockIdx.x * rows * kCopyRows + row;
   const char* src[2][kCopyRows];
   char* dst[2][kCopyRows];
   bool move[kCopyRows], hole[kCopyRows];
@@ -476,11 +480,14 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t stream) {
   if ((e = hipGetLastError()) != hipSuccess) return e;
   const int size = a.from.dtype == LSSVM_F32 ? 4 : 2;
   const int lanes = (int)a.from.dim * size / 16, rows = kThreads / lanes * kCopyRows;
-  const int64_t n = std::min<int64_t>(a.budget, most);
-  k_evict_copy<<<dim3((unsigned)((n + rows - 1) / rows), (unsigned)a.from.heads,
-                             (unsigned)a.from.sequences),
-                        kThreads, 0, stream>>>(a, lanes, size);
-  return hipGetLastError();
+  const int64_t n = std::min<int64_t>(a.budget, most), piece = rows * kMostBlocks;
+  for (int64_t row = 0; row < n; row += piece) {
+    const int64_t blocks = (std::min(n - row, piece) + rows - 1) / rows;
+    k_evict_copy<<<dim3((unsigned)blocks, (unsigned)a.from.heads, (unsigned)a.from.sequences),
+                   kThreads, 0, stream>>>(a, (int)row, lanes, size);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  return e;
 }
 
 }  // namespace lssvm

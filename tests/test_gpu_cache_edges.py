@@ -187,3 +187,55 @@ def test_scores_of_minus_infinity(torch_dev, dtype, new, L, page):
     others = [x for x in range(d) if x not in (5, 6, 7, 9, 10)]
     only = v[L - new, others].double()
     assert bool(((y[:, others].double() - only).abs() <= 8 * U * only.abs()).all())
+
+
+# ---------------------------------------------------------- largest sizes ---
+
+def test_evict_to_the_largest_budget(torch_dev):
+    """A budget of 2^29 keys of 512 bytes: 2^32 pieces of 16 bytes, of which a grid's side
+    cannot have a thread each. The sequence itself is short."""
+    torch, dev = torch_dev
+    import paper_2202_12674_amd as P
+    page, d, L = 1 << 12, 128, 9
+    columns = (1 << 29) // page
+    pool = torch.zeros(2, 2, 1, page, d, device=dev)
+    pool[:, 0, 0, :L] = torch.randn(2, L, d, device=dev)
+    weight = torch.zeros(2, 1, page, device=dev)
+    weight[0, 0, :L] = torch.arange(L, device=dev)
+    cache, target = (P.PagedCache(pool[0], pool[1],
+                                  torch.full((1, columns), i, dtype=torch.int32, device=dev),
+                                  torch.tensor([L * (1 - i)], dtype=torch.int32, device=dev), weight)
+                     for i in (0, 1))
+    kept = P.cache_evict(cache, target, 1 << 29, 0)
+    assert kept[0, 0, :L].tolist() == list(range(L)) and int(target.lengths) == L
+    assert bool((kept[0, 0, L:] == -1).all())
+    assert torch.equal(pool[:, 1, 0, :L], pool[:, 0, 0, :L]) and not pool[:, 1, 0, L:].any()
+    assert torch.equal(weight[1], weight[0])
+    del kept
+    torch.cuda.empty_cache()
+
+
+def test_evict_of_the_longest_sequence(torch_dev):
+    """2^29 keys, all recent: what stands first and last of them arrives there. Every page
+    is the same one, and all but two of the target's are holes."""
+    torch, dev = torch_dev
+    import paper_2202_12674_amd as P
+    page, d = 1 << 12, 128
+    columns = (1 << 29) // page
+    pool = torch.zeros(2, 3, 1, page, d, device=dev)
+    pool[:, 0] = torch.randn(2, 1, page, d, device=dev)
+    weight = torch.zeros(3, 1, page, device=dev)
+    weight[0, 0] = torch.rand(page, device=dev)
+    to = torch.full((1, columns), -1, dtype=torch.int32, device=dev)
+    to[0, 0], to[0, -1] = 1, 2
+    cache = P.PagedCache(pool[0], pool[1], torch.zeros_like(to),
+                         torch.full((1,), 1 << 29, dtype=torch.int32, device=dev), weight)
+    target = P.PagedCache(pool[0], pool[1], to, torch.zeros(1, dtype=torch.int32, device=dev),
+                          weight)
+    kept = P.cache_evict(cache, target, 1 << 29, 1 << 29)
+    assert int(target.lengths) == 1 << 29
+    assert int(kept[0, 0, 0]) == 0 and bool((kept[0, 0].diff() == 1).all())
+    for p in (1, 2):
+        assert torch.equal(pool[:, p], pool[:, 0]) and torch.equal(weight[p], weight[0])
+    del kept
+    torch.cuda.empty_cache()
