@@ -29,12 +29,14 @@ AttentionPlan make_plan(const lssvm_cache& c, int64_t tokens, int heads, bool ac
   // (8 of 2000 x 128: 64 rows 48, 84, 1024 rows 241, 304; 2 of 6000 x 256, 8000 rows 915,
   // 976) until a head's keys and values outgrow an XCD's L2, from which every tile reads
   // them (16000 x 96, 4096 rows: 734, 474; 8192 x 128, 8192 rows: 2262, 2110).
+  // (Tiles of 16 of the largest calls would be more than a grid holds: partly empty ones
+  // add 2^22 at most to those here.)
   const int64_t rows = tokens * group / c.sequences;
   if (c.dtype == LSSVM_F32)
-    p.few = (rows <= 256 || c.dim > 128 || most * c.dim * 8 <= kL2Bytes) &&
-            tokens * heads / 16 < kMostGroups;
+    p.few = rows <= 256 || c.dim > 128 || most * c.dim * 8 <= kL2Bytes;
   else
     p.few = rows <= (c.dim <= 64 ? 64 : c.dim <= 128 ? 16 : 8);
+  p.few &= tokens * heads / 16 < kMostGroups;
   p.rows = p.few ? 16 : 128;
   // every sequence's last tile may be partly empty
   p.tiles = tokens * group / p.rows + std::min(c.sequences, tokens);

@@ -239,3 +239,32 @@ def test_evict_of_the_longest_sequence(torch_dev):
         assert torch.equal(pool[:, p], pool[:, 0]) and torch.equal(weight[p], weight[0])
     del kept
     torch.cuda.empty_cache()
+
+
+def test_attention_of_as_many_rows_as_a_call_may_have(torch_dev):
+    """1024 sequences of 64 rows and 4096 heads, which in tiles of 16 rows would be more
+    workgroups than a grid holds. Every sequence has the same two keys."""
+    torch, dev = torch_dev
+    import paper_2202_12674_amd as P
+    seqs, new, heads, d = 1024, 64, 4096, 8
+    g = torch.Generator().manual_seed(6)
+    k, v = (torch.randn(1, heads, 16, d, generator=g).bfloat16().to(dev) for _ in "kv")
+    cache = P.PagedCache(k, v, torch.zeros(seqs, 1, dtype=torch.int32, device=dev),
+                         torch.full((seqs,), 2, dtype=torch.int32, device=dev))
+    off = (new * torch.arange(seqs + 1, device=dev)).int()
+    q = torch.randn(1, heads, d, generator=g).bfloat16().to(dev)
+    out = torch.full((seqs * new, heads, d), 7.0, dtype=torch.bfloat16, device=dev)
+    P.attention(q.expand(seqs * new, heads, d), cache, off, causal=False, out=out)
+    one = P.PagedCache(k, v, cache.table[:1], cache.lengths[:1])
+    want = P.attention(q.expand(new, heads, d), one, off[:2], causal=False)
+    p = torch.softmax(d ** -0.5 * (q[0, :, None].double() * k[0, :, :2].double()).sum(-1), -1)
+    exact = (p[..., None] * v[0, :, :2].double()).sum(1)
+    size = (p[..., None] * v[0, :, :2].double().abs()).sum(1)
+    # half a step of bf16 for the result and one for the weights
+    bound = 2.0 ** -8 * (exact.abs() + size) * 1.01 + 1e-6
+    assert bool(((want.double() - exact).abs() <= bound).all())
+    assert bool(((out[0].double() - exact).abs() <= bound).all())
+    for rows in out.split(1 << 12):
+        assert torch.equal(rows, out[:1].expand_as(rows))
+    del out, rows
+    torch.cuda.empty_cache()
