@@ -268,3 +268,31 @@ def test_attention_of_as_many_rows_as_a_call_may_have(torch_dev):
         assert torch.equal(rows, out[:1].expand_as(rows))
     del out, rows
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("pairs,interleaved", [(0, False), (3, True)])
+def test_append_of_as_many_tokens_as_a_call_may_have(torch_dev, pairs, interleaved):
+    """2^30 tokens of four and five pieces of 16 bytes each, 2^32 and more; all but the
+    last three lie outside the offsets."""
+    torch, dev = torch_dev
+    import paper_2202_12674_amd as P
+    tokens, d = 1 << 30, 8
+    k, v = (torch.arange(1.0, d + 1, device=dev).mul(s).view(1, 1, d) for s in (1, -2))
+    pool = torch.zeros(2, 1, 1, 16, d, device=dev)
+    weight = torch.ones(1, 1, 16, device=dev)
+    cache = P.PagedCache(pool[0], pool[1], torch.zeros(1, 1, dtype=torch.int32, device=dev),
+                         torch.tensor([5], dtype=torch.int32, device=dev), weight)
+    off = torch.tensor([tokens - 3, tokens], dtype=torch.int32, device=dev)
+    turned = {}
+    if pairs:       # every angle is 0
+        turned = dict(positions=torch.zeros(1, dtype=torch.int32, device=dev).expand(tokens),
+                      freqs=torch.ones(pairs, dtype=torch.float64, device=dev),
+                      interleaved=interleaved)
+        turned["positions"] = turned["positions"].contiguous()
+    P.cache_append(cache, k.expand(tokens, 1, d), v.expand(tokens, 1, d), off, **turned)
+    assert torch.equal(pool[0, 0, 0, 2:5], k[0].expand(3, d))
+    assert torch.equal(pool[1, 0, 0, 2:5], v[0].expand(3, d))
+    assert not pool[:, 0, 0, :2].any() and not pool[:, 0, 0, 5:].any()
+    assert weight.flatten().tolist() == [1.0] * 2 + [0.0] * 3 + [1.0] * 11
+    del turned
+    torch.cuda.empty_cache()
