@@ -296,3 +296,34 @@ def test_append_of_as_many_tokens_as_a_call_may_have(torch_dev, pairs, interleav
     assert weight.flatten().tolist() == [1.0] * 2 + [0.0] * 3 + [1.0] * 11
     del turned
     torch.cuda.empty_cache()
+
+
+# --------------------------------------------------------------- gradients ---
+
+def test_calls_that_would_lose_a_gradient_are_refused(torch_dev):
+    torch, dev = torch_dev
+    import paper_2202_12674_amd as P
+    cache = one_sequence(torch, dev, *torch.randn(2, 20, 64).bfloat16())
+    target = one_sequence(torch, dev, *torch.randn(2, 20, 64).bfloat16())
+    leaf = P.PagedCache(cache.k.clone().requires_grad_(), cache.v, cache.table, cache.lengths,
+                        cache.weight)
+    off = torch.tensor([0, 2], dtype=torch.int32, device=dev)
+    x = torch.randn(2, 1, 64, device=dev).bfloat16()
+    g = x.clone().requires_grad_()
+    pos, f = torch.arange(2, device=dev), P.rotary_frequencies(64, device=dev)[0]
+    calls = [lambda x, c: P.rotary(x, pos, f), lambda x, c: P.attention(x, c, off),
+             lambda x, c: P.cache_append(c, x, x, off, pos, f)]
+    for call in calls:
+        for a, c in [(g, cache)] + ([(x, leaf)] if call is not calls[0] else []):
+            with pytest.raises(ValueError, match="gradient"):
+                call(a, c)
+            with torch.no_grad():
+                call(a, c)
+        call(g.detach(), cache), call(x, cache)
+    with pytest.raises(ValueError, match="gradient"):
+        P.rotary(x, pos, f, out=g * 1)
+    with pytest.raises(ValueError, match="gradient"):
+        P.cache_evict(leaf, target, 4)
+    with torch.no_grad():
+        assert torch.equal(P.rotary(g, pos, f), P.rotary(x, pos, f))
+        P.cache_evict(leaf, target, 4)
