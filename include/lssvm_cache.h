@@ -87,7 +87,8 @@ int lssvm_rotary_frequencies(int64_t pairs, double base, int32_t scaling, double
  *
  * x, out       device, tokens x heads x dim values of dtype; strides of token and
  *              head in elements (host, 2 each), the dim values contiguous. out may be
- *              x itself with the same strides, else they must not overlap.
+ *              x itself with the same strides, else no rows of theirs may overlap
+ *              (nor, of other strides, all that lies between their first and last).
  * positions    device, tokens integers of position_bytes (4 or 8) bytes; any sign and
  *              size (from 2^53 on as the nearest double). An infinite angle gives NaN.
  * freqs        device, pairs doubles, 0 <= 2 * pairs <= dim. The first 2 * pairs values
@@ -138,7 +139,7 @@ size_t lssvm_attention_workspace_bytes(const lssvm_cache* cache, int64_t tokens,
  * group, always summed in one order.
  *
  * q, out      device, tokens x heads x dim values of the cache's dtype, strides of
- *             token and head (host, 2 each); they must not overlap.
+ *             token and head (host, 2 each); they must not overlap, as in lssvm_rotary.
  * heads       query heads, a multiple of the cache's heads, at most 65535.
  * offsets     as in lssvm_cache_append.
  * weight_out  where weight + gain goes, for the keys j < L of every sequence and

@@ -104,14 +104,31 @@ int check_out(const char* name, const void* p, const int64_t* stride, int64_t to
   return LSSVM_OK;
 }
 
-// Bytes from the first to behind the last value of rows.
+// Whether rows at a and b may share a value; those at b are apart. Of equal strides, as of
+// views of one array, it is known: rows i tokens and j heads from each other do if that
+// leaves less than a row between their starts, and since a stride steps over all that lies
+// within it, only the two multiples next to the distance can. Else it goes by all that
+// lies between the first and the last value.
 bool overlap(const void* a, const int64_t* as, const void* b, const int64_t* bs, int64_t tokens,
              int64_t heads, int64_t dim, int64_t size) {
   const auto span = [&](const int64_t* s) {
-    return (uintptr_t)((s[0] * (tokens - 1) + s[1] * (heads - 1) + dim) * size);
+    return (s[0] * (tokens - 1) + s[1] * (heads - 1) + dim) * size;
   };
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + span(bs) && y < x + span(as);
+  const int64_t apart_by = (int64_t)(reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(a));
+  if (apart_by >= span(as) || -apart_by >= span(bs)) return false;
+  if (apart_by % size || (tokens > 1 && as[0] != bs[0]) || (heads > 1 && as[1] != bs[1])) return true;
+  struct { int64_t stride, count; } outer{bs[0], tokens}, inner{bs[1], heads};
+  if (outer.count == 1 || (inner.count > 1 && outer.stride < inner.stride)) std::swap(outer, inner);
+  const auto near = [](auto d, int64_t left, auto use) {   // (of a single row, its own place)
+    if (d.count == 1) return use(left);
+    const int64_t low = left / d.stride - (left % d.stride < 0);
+    for (int64_t n = low; n <= low + 1; ++n)
+      if (std::abs(n) < d.count && use(left - n * d.stride)) return true;
+    return false;
+  };
+  return near(outer, apart_by / size, [&](int64_t left) {
+    return near(inner, left, [&](int64_t rest) { return std::abs(rest) < dim; });
+  });
 }
 
 int check_sizes(int64_t tokens, int64_t heads, int64_t dim) {

@@ -327,3 +327,38 @@ def test_calls_that_would_lose_a_gradient_are_refused(torch_dev):
     with torch.no_grad():
         assert torch.equal(P.rotary(g, pos, f), P.rotary(x, pos, f))
         P.cache_evict(leaf, target, 4)
+
+
+# ------------------------------------------------------- views of one array ---
+
+def test_results_beside_their_inputs_in_one_array(torch_dev):
+    """Inputs and results that are parts of every row of one array do not overlap, those
+    that share a value do."""
+    torch, dev = torch_dev
+    import paper_2202_12674_amd as P
+    g = torch.Generator().manual_seed(8)
+    heads, d, tokens = 3, 64, 7
+    wide = torch.randn(tokens, 2 * heads + 1, d, generator=g).bfloat16().to(dev)
+    x, y = wide[:, :heads], wide[:, heads + 1:]
+    keep = wide.clone()
+    pos, f = torch.arange(tokens, device=dev), P.rotary_frequencies(d, device=dev)[0]
+    k, v = torch.randn(2, 50, d, generator=g).bfloat16()
+    cache = one_sequence(torch, dev, k, v)
+    off = torch.tensor([0, tokens], dtype=torch.int32, device=dev)
+    for a, b in ((x, y), (y, x)):
+        wide.copy_(keep)
+        want = P.rotary(a, pos, f), P.attention(a, cache, off)
+        for i, call in enumerate((lambda: P.rotary(a, pos, f, out=b),
+                                  lambda: P.attention(a, cache, off, out=b))):
+            call()
+            assert torch.equal(b, want[i])
+        rest = slice(0, heads + 1) if b is y else slice(heads, None)
+        assert torch.equal(wide[:, rest], keep[:, rest])
+    with pytest.raises(P.LssvmError, match="overlap"):
+        P.rotary(x, pos, f, out=wide[:, 1:heads + 1])
+    with pytest.raises(P.LssvmError, match="overlap"):
+        P.attention(x, cache, off, out=wide[:, 2:heads + 2])
+    # the next token's row, some heads on
+    with pytest.raises(P.LssvmError, match="overlap"):
+        P.rotary(wide.view(-1, d)[:24].view(4, 6, d)[:3, :4], pos[:3], f,
+                 out=wide.view(-1, d)[3:21].view(3, 6, d)[:, :4])
