@@ -23,7 +23,8 @@
  * Rows (tokens x heads) of one call are at most 2^30, their values at most 2^33.
  *
  * dtype (of k, v, x, q and out) is LSSVM_F32, LSSVM_BF16 or LSSVM_F16. Sums, softmax
- * statistics, weights and rotation factors are fp32, angles fp64.
+ * statistics, weights and rotation factors are fp32, angles fp64. Scales are finite in
+ * fp32.
  */
 #ifndef LSSVM_CACHE_H_
 #define LSSVM_CACHE_H_

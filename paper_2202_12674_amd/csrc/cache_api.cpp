@@ -147,7 +147,7 @@ int check_angles(const void* positions, int32_t position_bytes, const double* fr
     return bad("position_bytes must be 4 or 8");
   if (pairs > 0 && (!aligned(positions, position_bytes) || !aligned(freqs, 8)))
     return bad("positions or freqs is not aligned");
-  if (!std::isfinite(scale)) return bad("scale must be finite");
+  if (!std::isfinite((float)scale)) return bad("scale must be finite in single precision");
   return LSSVM_OK;
 }
 
@@ -278,7 +278,8 @@ int lssvm_attention(const lssvm_cache* cache, const void* q, const int64_t* q_st
     return fail(LSSVM_EINVAL, "heads (%lld) must be a multiple of the cache's (%lld)",
                 (long long)heads, (long long)cache->heads);
   if (!offsets) return bad("offsets is NULL");
-  if (!std::isfinite(scale)) return bad("scale must be finite");
+  const float scale2 = (float)(scale * 1.4426950408889634074);   // exponents are of two
+  if (!std::isfinite(scale2)) return bad("scale must be finite in single precision");
   AttentionArgs a{};
   if (accumulate) {
     if (!cache->weight) return bad("accumulate needs a cache with weights");
@@ -311,7 +312,7 @@ int lssvm_attention(const lssvm_cache* cache, const void* q, const int64_t* q_st
   a.heads = (int)heads;
   a.group = (int)(heads / cache->heads);
   a.offsets = offsets;
-  a.scale2 = (float)(scale * 1.4426950408889634074);
+  a.scale2 = scale2;
   a.causal = causal != 0;
   a.accumulate = accumulate != 0;
   return launched(launch_attention(a, workspace, static_cast<hipStream_t>(stream)));
