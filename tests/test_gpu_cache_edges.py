@@ -362,3 +362,78 @@ def test_results_beside_their_inputs_in_one_array(torch_dev):
     with pytest.raises(P.LssvmError, match="overlap"):
         P.rotary(wide.view(-1, d)[:24].view(4, 6, d)[:3, :4], pos[:3], f,
                  out=wide.view(-1, d)[3:21].view(3, 6, d)[:, :4])
+
+
+# ------------------------------------- keys and queries that are not finite ---
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("new,page", [(1, 16), (9, 21), (200, 16)])
+def test_keys_and_queries_that_are_not_finite(torch_dev, dtype, new, page):
+    """A NaN in a key, an infinite score or a NaN in a query makes a NaN of every row that
+    it enters, and changes no other."""
+    torch, dev = torch_dev
+    import cache_oracle as O
+    import paper_2202_12674_amd as P
+    dt = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}[dtype]
+    g = torch.Generator().manual_seed(9)
+    L, d, heads = 333, 64, 2
+    k, v = (torch.randn(L, d, generator=g).to(dt) for _ in "kv")
+    q = torch.randn(new, heads, d, generator=g).to(dt)
+    q[:, 0, 7] = 1.0
+    q[:, 1, 7] = -1.0
+    last, pages = L - new // 3 - 1, -(-L // page)      # seen by the last third of the rows
+    table = torch.arange(pages, dtype=torch.int32)[None]
+    off = torch.tensor([0, new], dtype=torch.int32)
+
+    def plain(k, v):
+        pool = torch.zeros(2, pages * page, d, dtype=dt)
+        pool[0, :len(k)], pool[1, :len(k)] = k, v
+        pool = pool.view(2, pages, 1, page, d)
+        return O.attention(q, pool[0], pool[1], table, torch.tensor([len(k)]), off, 1.0, True)[:2]
+
+    want, bound = plain(k, v)
+    for what in ("nan key", "inf key", "nan query"):
+        kk, qq, out = k.clone(), q.clone(), want.clone()
+        rows = torch.arange(new) >= last - (L - new)
+        if what == "nan key":
+            kk[last, 7], out[rows] = math.nan, math.nan
+        elif what == "inf key":       # head 0: a score of infinity, head 1: of minus infinity
+            kk[last, 7], out[rows, 0] = math.inf, math.nan
+        else:
+            qq[new // 2, 1, 3], out[new // 2, 1] = math.nan, math.nan
+        y = attend(torch, dev, qq, kk, v, page, causal=True)[0].double()
+        slack = bound.clone()
+        if what == "inf key":         # as without that key, for the rows that see it
+            less = [torch.cat([x[:last], x[last + 1:]]) for x in (k, v)]
+            out[rows, 1], slack[rows, 1] = (x[rows, 1] for x in plain(*less))
+        fine = out.isfinite()
+        assert torch.equal(y.isnan(), out.isnan()), what
+        assert bool(((y - out).abs() <= slack)[fine].all()), what
+
+
+# ------------------------------------------------------------ wide tables ---
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("new", [[1, 1, 1], [1, 60, 3], [100, 40, 120]])
+@pytest.mark.parametrize("columns", [40, 900])
+def test_tables_much_wider_than_their_sequences(torch_dev, dtype, new, columns):
+    """Room for many times the keys that are there, in steps of one plan and another: as
+    in a table of just the sequences' pages, and prompts and single tokens in one call."""
+    torch, dev = torch_dev
+    import cache_oracle as O
+    import paper_2202_12674_amd as P
+    from test_gpu_cache import make, offsets_of, _check
+    lengths, page, d = [130, 61, 250], 16, 64
+    cache, (k, v, table, lens, w) = make(torch, dev, dtype, lengths, 2, d, page, 3, columns=columns)
+    q = torch.randn(sum(new), 6, d, generator=torch.Generator().manual_seed(3)).to(k.dtype)
+    off = offsets_of(torch, new)
+    wout = torch.full(w.shape, -5.0, device=dev)
+    y = P.attention(q.to(dev), cache, off.to(dev), accumulate=True, weight_out=wout)
+    want, bound, ww, slack = O.attention(q, k, v, table, lens, off, d ** -0.5, True, w)
+    _check(y, want, bound, "out")
+    there = ~w.isnan()
+    _check(wout.cpu()[there], ww[there], slack[there], "weight")
+    assert bool((wout.cpu()[~there] == -5.0).all())
+    target, _ = make(torch, dev, dtype, [40] * 3, 2, d, page, 4, columns=columns)
+    kept = P.cache_evict(cache, target, 40, 7)
+    assert torch.equal(kept.cpu(), O.evict(w, table, lens, 40, 7, page))
