@@ -37,7 +37,8 @@ struct AttentionArgs {
   // workspace
   float* lse;          // per row: log2 of the sum of exponentials (with weights)
   float* part;         // splits x rows x dim: sums of one split, and
-  float2* part_ml;     // ... its maximum and sum of exponentials (-1 where sees_any)
+  float2* part_ml;     // ... its maximum and sum of exponentials; the latter negative where
+                       // keys are seen, but all with scores of minus infinity
   float* scores;       // rows x pitch
 };
 
@@ -90,15 +91,6 @@ struct Tile {
 LSSVM_DEV int seen_keys(const AttentionArgs& a, const Tile& t, int r) {
   const int k = a.causal ? t.length - t.n + r / a.group + 1 : t.length;
   return k > 0 ? k : 0;
-}
-
-// Whether row r sees a key of [from, to) that is there. Asked of rows without a sum: all
-// that they see then has scores of minus infinity, and no softmax.
-LSSVM_DEV bool sees_any(const AttentionArgs& a, const Tile& t, int r, int from, int to) {
-  to = min(to, seen_keys(a, t, r));
-  for (int j = from, slot; j < to; j += (int)a.c.page - slot)
-    if (cache_page(a.c, t.s, j, &slot) >= 0) return true;
-  return false;
 }
 
 LSSVM_DEV void sequence_rows(const AttentionArgs& a, int s, int64_t* first, int* n) {

@@ -298,6 +298,7 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
   // others count only the values of one kind (below).
   f32x16 s[NB];
   float base, lift;
+  bool met = false;     // whether this lane's row sees any of the lane's keys
   bool taken = false;   // whether the pass without values that are not finite met any
   auto sweep = [&](int pass) {
     const Kind kind = (Kind)(pass - 1);
@@ -339,10 +340,12 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
               s[b][i] = kind != Kind::lost || s[b][i] == -INFINITY ? 0.0f : -INFINITY;
             if constexpr (kShort<T>) low = sees ? fminf(low, s[b][i]) : low;
             if (!sees) s[b][i] = -INFINITY;
+            met |= sees;
           }
           look_at(b);
         }
       } else {
+        met = true;
         look_at(NB - 1);
         if constexpr (kShort<T>)
 #pragma unroll
@@ -510,10 +513,11 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
   const int64_t rows = a.tokens * a.heads;
   auto write = [&](Kind kind) {
     const int y = wave * 32 + c;
+    // no softmax, unless other splits have one
+    if (met && top == -INFINITY && l == 0.0f) l = -1.0f;
     float sum = l + __shfl_xor(l, 32);
     if (y >= t.rows) return;
-    if (sum == 0.0f && sees_any(a, t, t.row0 + y, block0 * KEYS, block1 * KEYS))
-      sum = used == 1 ? __builtin_nanf("") : -1.0f;
+    if (sum < 0.0f && used == 1) sum = __builtin_nanf("");
     const int r = t.row0 + y, tok = r / a.group, head = hk * a.group + r % a.group;
     const int64_t at = (t.first + tok) * a.heads + head;
     T* out = static_cast<T*>(a.out) + (t.first + tok) * a.os.outer + head * a.os.head;

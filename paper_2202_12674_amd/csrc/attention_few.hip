@@ -235,6 +235,7 @@ __global__ void __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) k_attention_few
 
   f32x4 o[NC * CE];
   float top, l;
+  bool met = false;   // whether this lane's row sees any of the lane's keys
   const float lift_again = lowered<T>(few_lift<T>, 0, t.keys);
 
   // O^T += V^T p for the step's values: `hi` and `lo` are the 16-bit parts of p, in fp32
@@ -340,7 +341,12 @@ __global__ void __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) k_attention_few
         for (int b = 0; b < KB; ++b)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (16 * b + i >= lim - j0 - 4 * g || !(there >> (4 * b + i) & 1)) s[b][i] = -INFINITY;
+            if (16 * b + i >= lim - j0 - 4 * g || !(there >> (4 * b + i) & 1))
+              s[b][i] = -INFINITY;
+            else
+              met = true;
+      } else {
+        met = true;
       }
       if (a.plan.pitch && m < t.rows) {
 #pragma unroll
@@ -442,6 +448,8 @@ __global__ void __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) k_attention_few
   if (__any(!safe)) sweep(std::true_type{});
 
   // join the waves' sums
+  // no softmax, unless other waves or splits have one
+  if (met && top == -INFINITY && l == 0.0f) l = -1.0f;
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
   if (g == 0) sum_m[wave][m] = top, sum_l[wave][m] = l;
@@ -474,11 +482,13 @@ __global__ void __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) k_attention_few
       high = fmaxf(high, sum_m[w][y]);
     }
     float total = 0.0f;
+    bool any = false;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w)
+    for (int w = 0; w < kWaves; ++w) {
       total += sum_l[w][y] * __builtin_amdgcn_exp2f(sum_m[w][y] - (high == -INFINITY ? 0.0f : high));
-    if (total == 0.0f && sees_any(a, t, t.row0 + y, block0 * KEYS, block1 * KEYS))
-      total = last ? __builtin_nanf("") : -1.0f;
+      any |= sum_l[w][y] < 0.0f;
+    }
+    if (total == 0.0f && any) total = last ? __builtin_nanf("") : -1.0f;
     const int tok = (t.row0 + y) / a.group, h = hk * a.group + (t.row0 + y) % a.group;
     const int64_t at = (t.first + tok) * a.heads + h;
     if (last) {

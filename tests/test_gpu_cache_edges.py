@@ -401,8 +401,9 @@ def test_keys_and_queries_that_are_not_finite(torch_dev, dtype, new, page):
             kk[last, 7], out[rows, 0] = math.inf, math.nan
         else:
             qq[new // 2, 1, 3], out[new // 2, 1] = math.nan, math.nan
-        y = attend(torch, dev, qq, kk, v, page, causal=True)[0].double()
-        slack = bound.clone()
+        y, w = attend(torch, dev, qq, kk, v, page, causal=True, accumulate=True)
+        y, slack = y.double(), bound.clone()
+        assert bool(w.isnan()[:L - new + 1].all()), what     # seen by every row
         if what == "inf key":         # as without that key, for the rows that see it
             less = [torch.cat([x[:last], x[last + 1:]]) for x in (k, v)]
             out[rows, 1], slack[rows, 1] = (x[rows, 1] for x in plain(*less))
