@@ -18,19 +18,9 @@ constexpr int64_t kMostBlocks = 1 << 23;
 // cos and sin of `angle`, to about an ulp of fp32: the quarter turns are taken off in
 // fp64 (pi/2 in two parts), so that positions of millions lose nothing; what is left is
 // at most pi/4, where the Taylor polynomials of degree 9 and 10 are off by 2e-9 and 2e-10.
-// From 2^45 on, where the rounding of k shows in what is left, sincos reduces the angle,
-// whatever its size. Here, per angle, it costs the others a branch (9 x 2048 tokens
-// appended 31.3 -> 31.7 us); apart from them, for a thread's angles one after the other,
-// its registers cost more (36.3 us).
+// From kFarAngle = 2^45 on the rounding of k shows in what is left (turn_far).
 constexpr double kFarAngle = 35184372088832.0;
 LSSVM_DEV void turn(double angle, float* c, float* s) {
-  if (fabs(angle) >= kFarAngle) {
-    double ds, dc;
-    sincos(angle, &ds, &dc);
-    *c = (float)dc;
-    *s = (float)ds;
-    return;
-  }
   const double k = rint(angle * 0.63661977236758134308);
   double rest = fma(-k, 1.57079632679489655800, angle);
   rest = fma(-k, 6.12323399573676603587e-17, rest);
@@ -57,26 +47,55 @@ __host__ __device__ inline int copy_chunks(int values) {
   return (values + kVec<T> - 1) / kVec<T>;
 }
 
+LSSVM_DEV double position(const RotaryArgs& a, int64_t t) {
+  return a.wide_positions ? (double)static_cast<const int64_t*>(a.positions)[t]
+                          : (double)static_cast<const int32_t*>(a.positions)[t];
+}
+
 // The factors of the pairs of chunk `at` (of its last pair behind the last one).
 template <typename T, bool INTER>
 struct Factors {
   static constexpr int N = INTER ? kVec<T> / 2 : kVec<T>;
   float c[N], s[N];
-  LSSVM_DEV void set(const RotaryArgs& a, int64_t t, int at) {
+  // false if an angle is too far for them
+  LSSVM_DEV bool set(const RotaryArgs& a, int64_t t, int at) {
     double f[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) f[i] = a.freqs[min(at * N + i, a.pairs - 1)];
-    const double p = a.wide_positions
-                         ? (double)static_cast<const int64_t*>(a.positions)[t]
-                         : (double)static_cast<const int32_t*>(a.positions)[t];
+    const double p = position(a, t);
+    bool near = true;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
+      near &= fabs(p * f[i]) < kFarAngle;
       turn(p * f[i], &c[i], &s[i]);
       c[i] *= a.scale;
       s[i] *= a.transpose ? -a.scale : a.scale;
     }
+    return near;
   }
 };
+
+// The pairs of chunk `at` of every groups-th head, with sincos, which reduces angles of
+// any size: a path of its own, so that the others' registers and code do not grow by it
+// (within `turn` small calls took 0.6 us more).
+template <typename T, bool INTER>
+LSSVM_DEV void turn_far(const RotaryArgs& a, int64_t t, int at, const T* x, T* y, int64_t y_head,
+                        int group, int groups) {
+  constexpr int N = Factors<T, INTER>::N;
+#pragma unroll 1
+  for (int i = at * N; i < min(at * N + N, a.pairs); ++i) {
+    double ds, dc;
+    sincos(position(a, t) * a.freqs[i], &ds, &dc);
+    const float c = (float)dc * a.scale, s = (float)ds * (a.transpose ? -a.scale : a.scale);
+    const int m = INTER ? 2 * i : i, n = INTER ? 2 * i + 1 : i + a.pairs;
+#pragma unroll 1
+    for (int h = group; h < a.heads; h += groups) {
+      const float p = (float)x[h * a.xs.head + m], q = (float)x[h * a.xs.head + n];
+      y[h * y_head + m] = (T)(p * c - q * s);
+      y[h * y_head + n] = (T)(q * c + p * s);
+    }
+  }
+}
 
 // Chunk `at` of the pairs of one head: read, turned, written. All of it is read before
 // any is written, so y may be x.
@@ -192,7 +211,10 @@ __global__ void __launch_bounds__(kThreads) k_rotary(RotaryArgs a, int chunks, i
   Pairs<T, INTER> now, next;
   now.read(x + group * a.xs.head, at, a.pairs);
   Factors<T, INTER> f;
-  f.set(a, t, at);
+  if (!f.set(a, t, at)) {
+    turn_far<T, INTER>(a, t, at, x, y, a.os.head, group, groups);
+    return;
+  }
   for (int h = group; h < a.heads; h += groups) {
     if (h + groups < a.heads) next.read(x + (h + groups) * a.xs.head, at, a.pairs);
     now.turn(f);
@@ -231,9 +253,10 @@ __global__ void __launch_bounds__(kThreads) k_append(AppendArgs a, unsigned from
   const T* xv = static_cast<const T*>(a.v) + t * a.vs.outer;
   Factors<T, INTER> f;
   Pairs<T, INTER> pairs;
+  bool near = true;
   if (at < turned) {
     pairs.read(xk + group * a.k.xs.head, at, a.k.pairs);
-    f.set(a.k, t, at);
+    near = f.set(a.k, t, at);
   }
   // the sequence: the last whose first token is not behind t
   int lo = 0, hi = held;
@@ -256,6 +279,10 @@ __global__ void __launch_bounds__(kThreads) k_append(AppendArgs a, unsigned from
   if (page < 0) return;
   T* k = static_cast<T*>(a.c.k) + page * a.c.k_stride[0] + slot * a.c.k_stride[2];
   T* v = static_cast<T*>(a.c.v) + page * a.c.v_stride[0] + slot * a.c.v_stride[2];
+  if (!near) {
+    turn_far<T, INTER>(a.k, t, at, xk, k, a.c.k_stride[1], group, groups);
+    return;
+  }
   for (int h = group; h < a.k.heads; h += groups) {
     if (at < turned) {
       if (h != group) pairs.read(xk + h * a.k.xs.head, at, a.k.pairs);
