@@ -94,12 +94,11 @@ def _gpu(t, name: str, dims: int, dtype=None, device=None):
     return t
 
 
-def _no_gradient(*tensors) -> None:
+def _no_gradient(requires_grad: bool) -> None:
     """An error where autograd would be asked to record a call: nothing does that here."""
-    for t in tensors:
-        if t.requires_grad and _torch().is_grad_enabled():
-            raise ValueError("these calls record no gradient: pass detached tensors or call under "
-                             "torch.no_grad() (the gradient of rotary is rotary with transpose)")
+    if requires_grad and _torch().is_grad_enabled():
+        raise ValueError("these calls record no gradient: pass detached tensors or call under "
+                         "torch.no_grad() (the gradient of rotary is rotary with transpose)")
 
 
 @functools.cache
@@ -187,7 +186,7 @@ def _offsets(t, cache):
 def _angles(positions, freqs, tokens: int, device):
     """(positions, bytes of one, freqs, pairs) for the library."""
     torch = _torch()
-    _no_gradient(_gpu(freqs, "freqs", 1, torch.float64, device))
+    _no_gradient(_gpu(freqs, "freqs", 1, torch.float64, device).requires_grad)
     _gpu(positions, "positions", 1, None, device)
     if positions.dtype not in (torch.int32, torch.int64):
         raise TypeError(f"positions must be int32 or int64, not {positions.dtype}")
@@ -236,8 +235,8 @@ def rotary(x, positions, freqs, scale: float = 1.0, interleaved: bool = False,
         _gpu(out, "out", 3, x.dtype, x.device)
         if out.shape != x.shape:
             raise ValueError(f"out must have the shape of x, {tuple(x.shape)}")
-        _no_gradient(out)
-    _no_gradient(x)
+        _no_gradient(out.requires_grad)
+    _no_gradient(x.requires_grad)
     tokens, heads, dim = x.shape
     _call(x.device, _lib().lssvm_rotary, x.data_ptr(), _two(*x.stride()), out.data_ptr(),
           _two(*out.stride()), tokens, heads, dim,
@@ -260,7 +259,8 @@ def cache_append(cache, k, v, offsets, positions=None, freqs=None, scale: float 
         raise ValueError("k and v must have the same tokens")
     if (positions is None) != (freqs is None):
         raise ValueError("positions and freqs are given together")
-    _no_gradient(k, v, cache.k, cache.v)
+    _no_gradient(k.requires_grad or v.requires_grad or cache.k.requires_grad or
+                 cache.v.requires_grad)
     angles = (None, 0, None, 0) if freqs is None else _angles(positions, freqs, tokens,
                                                               cache.device)
     _call(cache.device, _lib().lssvm_cache_append, cache._ref, k.data_ptr(), _two(*k.stride()),
@@ -293,8 +293,8 @@ def attention(q, cache, offsets, scale: float | None = None, causal: bool = True
         _rows(out, "out", cache, heads)
         if out.shape[0] != tokens:
             raise ValueError(f"out must have the shape of q, {tuple(q.shape)}")
-        _no_gradient(out)
-    _no_gradient(q, cache.k, cache.v)
+        _no_gradient(out.requires_grad)
+    _no_gradient(q.requires_grad or cache.k.requires_grad or cache.v.requires_grad)
     w = None
     if weight_out is not None:
         if not accumulate:
@@ -328,7 +328,7 @@ def cache_evict(cache, target, budget: int, recent: int = 0, kept=None):
     _cache(target, "target")
     if target.device != cache.device:
         raise ValueError(f"target must be on {cache.device}, not {target.device}")
-    _no_gradient(cache.k, cache.v, cache.weight, target.k, target.v)
+    _no_gradient(any(t.requires_grad for c in (cache, target) for t in (c.k, c.v)))
     shape = (cache.sequences, cache.heads, budget)
     if kept is None:
         kept = torch.empty(shape, dtype=torch.int32, device=cache.device) if budget > 0 else None
