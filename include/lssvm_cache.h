@@ -24,7 +24,9 @@
  *
  * dtype (of k, v, x, q and out) is LSSVM_F32, LSSVM_BF16 or LSSVM_F16. Sums, softmax
  * statistics, weights and rotation factors are fp32, angles fp64. Scales are finite in
- * fp32.
+ * fp32. In 16-bit types attention's probabilities are rounded to the type where tiles of
+ * many rows multiply them with the values (half a step each, of fp16 down to 2^-50 of the
+ * largest), and enter in two parts where rows are few.
  */
 #ifndef LSSVM_CACHE_H_
 #define LSSVM_CACHE_H_
@@ -72,7 +74,9 @@ enum {
                               stretched by factor, the fastest not at all                  */
     LSSVM_ROPE_YARN = 3    /* by parts: pairs of 32 turns or more over `original` positions
                               as they are, of 1 or fewer divided by factor, between them
-                              linearly mixed; values times 0.1 ln(factor) + 1              */
+                              mixed linearly in their turns (not in their index, as some
+                              models do: those bring frequencies of their own); values
+                              times 0.1 ln(factor) + 1                                     */
 };
 
 /* Writes the `pairs` frequencies (host, fp64) of rotary positions and the factor of
@@ -123,7 +127,9 @@ int lssvm_cache_append(const lssvm_cache* cache, const void* k, const int64_t* k
                        void* stream);
 
 /* Device workspace of lssvm_attention for `tokens` rows of `heads` heads; 0 if an
- * argument is out of range. */
+ * argument is out of range. With accumulate and few rows (tokens x group up to 32 per
+ * sequence) it holds 4 bytes per row and key of columns * page: a table no wider than
+ * its sequences need takes less. */
 size_t lssvm_attention_workspace_bytes(const lssvm_cache* cache, int64_t tokens, int64_t heads,
                                        int32_t accumulate);
 

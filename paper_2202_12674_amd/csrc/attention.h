@@ -56,9 +56,9 @@ constexpr int kFewLeast = 4, kChunkLeast = 4;
 // those that still lie below 2^kFaint are multiplied apart, kFar exponents higher, in steps
 // that have any. Full rounding then holds down to 2^-50 of the largest weight. Sums are
 // lifted alike, maxima lowered by as much where they leave a kernel. 2 x 2048 rows over
-// 8192 keys, 16/4 heads of 128: 417 us with scores of deviation 1.5, where hardly a step
-// has faint ones; 633 with 6, where most have (bf16 424, 430). 64 single tokens over
-// 16384 keys: 705 and 716.
+// 8192 keys, 16/4 heads of 128: 409 us with scores of deviation 1.5, where hardly a step
+// has faint ones; 618 with 6, where most have (bf16 383, 389). 64 single tokens over
+// 16384 keys: 706 either way.
 template <typename T>
 constexpr bool kShort = std::is_same_v<T, f16_t>;
 template <typename T>

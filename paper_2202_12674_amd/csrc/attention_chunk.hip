@@ -132,10 +132,10 @@ LSSVM_DEV int column_at(int d, int keys8) { return d * 128 + 16 * (keys8 ^ ((d ^
 // as the values themselves were; its sum is taken before that. fp16 has too short a
 // range for that: small ones are multiplied apart (attention.h).
 //
-// Measured: bf16, 4 x 2048 rows x 32 heads over 16384 keys, 128 wide: 1.69 ms, 780
-// TFLOP/s (a large library product reaches 1107). The matrix cores are busy for 34% of
-// it, at 2.1 GHz; without loading (the same tile over and over) it takes 1.33 ms, and
-// there a step of two workgroups is 2.1 us of which the two products make 0.75, the
+// Measured: bf16, 4 x 2048 rows x 32 heads over 16384 keys, 128 wide: 1.57 to 1.69 ms on
+// different cards, 780 to 837 TFLOP/s (a large library product reaches 1107). The matrix
+// cores are busy for 36% of it; without loading (the same tile over and over) the form of
+// 1.69 ms took 1.33, and there a step of two workgroups is 2.1 us of which the two products make 0.75, the
 // exponentials 0.3, and the rest waits in turn: for LDS, the maximum, the barrier. Two
 // blocks of 32 rows per wave, half a step apart in one instruction stream, took 2.9 ms:
 // the results do not fit the registers that vector instructions reach, and moving them
@@ -580,7 +580,7 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
 // weight_out = weight + the probabilities that the rows give to 64 keys, which stay in
 // registers: every wave takes every fourth 32 rows, forms the scores anew and sums
 // p = 2^(score - lse) per key; the waves' sums are joined in order. Measured: f16, 6 x
-// 700 rows x 14 heads over 3001 keys, 64 wide: 47 us (13.5 GFLOP); bound by reading the
+// 700 rows x 14 heads over 3001 keys, 64 wide: 49 us (13.5 GFLOP); bound by reading the
 // rows from L2, once for every 64 keys (32 keys: 70 us; rows not read ahead: 68).
 template <typename T, int D>
 __global__ void __launch_bounds__(256) k_weights_chunk(AttentionArgs a) {

@@ -191,7 +191,7 @@ LSSVM_DEV int64_t split(int64_t v, int by, int* rest) {
 }
 
 // Measured: bf16, 16384 tokens x 32 heads x 128, 268 MB, in 42 us (6.3 TB/s, in part from
-// the cache behind the L2s); fp32, 3001 x 12 x 80, 23 MB, in 6.5 us.
+// the cache behind the L2s); fp32, 3001 x 12 x 80, 23 MB, in 6.3 us.
 template <typename T, bool INTER>
 __global__ void __launch_bounds__(kThreads) k_rotary(RotaryArgs a, int chunks, int turned,
                                                      int groups) {
@@ -233,7 +233,7 @@ hipError_t by_dtype(int dtype, F f) {
 // -------------------------------------------------------- cache append ------
 
 // One chunk of a new token's key or value per thread, for some of its heads. Measured: 9
-// x 2048 tokens x 8 heads x 128, 110 MB, in 23 us (4.8 TB/s); 64 tokens in 5.6 us, a
+// x 2048 tokens x 8 heads x 128, 110 MB, in 24 us (4.6 TB/s); 64 tokens in 5.3 us, a
 // chain of loads (offsets, length, page).
 template <typename T, bool INTER>
 __global__ void __launch_bounds__(kThreads) k_append(AppendArgs a, unsigned from_block,
