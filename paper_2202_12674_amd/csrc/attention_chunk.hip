@@ -129,8 +129,10 @@ LSSVM_DEV int column_at(int d, int keys8) { return d * 128 + 16 * (keys8 ^ ((d ^
 // there once, 4 keys x 8 values per thread, so that a lane reads 8 keys of its column
 // in one piece; fp32 ones are read singly and stay in rows.
 // 16-bit types: p is rounded to the stored type for the product, half a step of it,
-// as the values themselves were; its sum is taken before that. fp16 has too short a
-// range for that: small ones are multiplied apart (attention.h).
+// as the values themselves were; its sum is taken before that. (In two parts, as for few
+// rows, the result's error is 1.7e-3 in place of 2.3e-3, and the time of the case below
+// 2.08 ms in place of 1.57.) fp16 has too short a range for that: small ones are
+// multiplied apart (attention.h).
 //
 // Measured: bf16, 4 x 2048 rows x 32 heads over 16384 keys, 128 wide: 1.57 to 1.69 ms on
 // different cards, 780 to 837 TFLOP/s (a large library product reaches 1107). The matrix
