@@ -141,7 +141,8 @@ size_t lssvm_attention_workspace_bytes(const lssvm_cache* cache, int64_t tokens,
  *     p_j = exp(scale <q, k_j>) / sum over the seen j of the same,  out = sum_j p_j v_j.
  * A row that sees no key gets zeros, one that sees only keys of score minus infinity
  * NaNs. A value that is not finite reaches the rows that see its key and no others: as
- * itself, or as a NaN under a score of minus infinity. Rows outside the offsets are left as they were.
+ * itself, or as a NaN under a score of minus infinity. Rows outside the offsets are left
+ * as they were.
  * With accumulate, each key's weight grows by the p_j of all rows and heads of its
  * group, always summed in one order.
  *

@@ -137,11 +137,11 @@ LSSVM_DEV int column_at(int d, int keys8) { return d * 128 + 16 * (keys8 ^ ((d ^
 // Measured: bf16, 4 x 2048 rows x 32 heads over 16384 keys, 128 wide: 1.57 to 1.69 ms on
 // different cards, 780 to 837 TFLOP/s (a large library product reaches 1107). The matrix
 // cores are busy for 36% of it; without loading (the same tile over and over) the form of
-// 1.69 ms took 1.33, and there a step of two workgroups is 2.1 us of which the two products make 0.75, the
-// exponentials 0.3, and the rest waits in turn: for LDS, the maximum, the barrier. Two
-// blocks of 32 rows per wave, half a step apart in one instruction stream, took 2.9 ms:
-// the results do not fit the registers that vector instructions reach, and moving them
-// costs more than the overlap gives.
+// 1.69 ms took 1.33, and there a step of two workgroups is 2.1 us of which the two
+// products make 0.75, the exponentials 0.3, and the rest waits in turn: for LDS, the
+// maximum, the barrier. Two blocks of 32 rows per wave, half a step apart in one
+// instruction stream, took 2.9 ms: the results do not fit the registers that vector
+// instructions reach, and moving them costs more than the overlap gives.
 template <typename T, int D>
 __global__ void __launch_bounds__(64 * kWaves, D > 128 ? 1 : 2)
     k_attention_chunk(AttentionArgs a) {
