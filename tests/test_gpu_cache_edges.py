@@ -83,6 +83,37 @@ def test_weights_of_all_sizes_in_half_precision(torch_dev, new, least):
     _faint(torch, dev, gaps.tolist(), v, new, 16)
 
 
+@pytest.mark.parametrize("new", [1, 9, 150])
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 21), (256, 32)])
+def test_small_weights_beside_values_that_are_not_finite(torch_dev, new, d, page):
+    """Half precision, causal rows: faint weights in steps that are masked, and gone over
+    again for the infinities and NaNs of the last tokens."""
+    torch, dev = torch_dev
+    import cache_oracle as O
+    g = torch.Generator().manual_seed(12)
+    L, pages = 700, -(-700 // page)
+    k, v = torch.zeros(L, d), 2e4 + 4e4 * torch.rand(L, d, generator=g)
+    k[:, 0], v[0] = -14.0 - 14.0 * torch.rand(L, generator=g), 0.0
+    k[0, 0] = 0.0
+    v[L - 1, 3], v[L - 1 - new // 2, 4], v[L - new, 5] = math.inf, math.nan, -math.inf
+    k, v = k.half(), v.half()
+    q = torch.zeros(new, 2, d).half()
+    q[..., 0] = 1.0
+    pool = torch.zeros(2, pages * page, d).half()
+    pool[0, :L], pool[1, :L] = k, v
+    pool = pool.view(2, pages, 1, page, d)
+    want, bound, w, slack = O.attention(
+        q, pool[0], pool[1], torch.arange(pages, dtype=torch.int32)[None], torch.tensor([L]),
+        torch.tensor([0, new], dtype=torch.int32), 1.0, True, torch.zeros(pages, 1, page))
+    y, weight = attend(torch, dev, q, k, v, page, causal=True, accumulate=True)
+    fine = want.isfinite()
+    # (the plain bound's absolute part, the least normal number, down to half a step there)
+    bound = bound - torch.finfo(torch.float16).tiny + 2.0 ** -24
+    assert torch.equal(y.double()[~fine].nan_to_num(7.0), want[~fine].nan_to_num(7.0))
+    assert bool(((y.double() - want).abs() <= bound)[fine].all())
+    assert bool(((weight - w.view(-1)[:L]).abs() <= slack.view(-1)[:L]).all())
+
+
 # ----------------------------------------------------------- wide angles ----
 
 @pytest.mark.parametrize("interleaved", [False, True])
