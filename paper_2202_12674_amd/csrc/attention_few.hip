@@ -407,7 +407,8 @@ __global__ void __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) k_attention_few
         }
         if constexpr (decltype(with_wild)::value) {
           auto seen = [&](int b, int i) {
-            const bool sees = !masked || (16 * b + i < lim - j0 - 4 * g && (there >> (4 * b + i) & 1));
+            const bool sees =
+                !masked || (16 * b + i < lim - j0 - 4 * g && (there >> (4 * b + i) & 1));
             return far || !sees ? 0.0f : s[b][i] == -INFINITY ? kCodeNan : 1.0f;
           };
           if constexpr (HALF) {
@@ -485,7 +486,8 @@ __global__ void __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) k_attention_few
     bool any = false;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      total += sum_l[w][y] * __builtin_amdgcn_exp2f(sum_m[w][y] - (high == -INFINITY ? 0.0f : high));
+      total +=
+          sum_l[w][y] * __builtin_amdgcn_exp2f(sum_m[w][y] - (high == -INFINITY ? 0.0f : high));
       any |= sum_l[w][y] < 0.0f;
     }
     if (total == 0.0f && any) total = last ? __builtin_nanf("") : -1.0f;

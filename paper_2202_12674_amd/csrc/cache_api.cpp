@@ -114,11 +114,13 @@ bool overlap(const void* a, const int64_t* as, const void* b, const int64_t* bs,
   const auto span = [&](const int64_t* s) {
     return (s[0] * (tokens - 1) + s[1] * (heads - 1) + dim) * size;
   };
-  const int64_t apart_by = (int64_t)(reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(a));
+  const int64_t apart_by = reinterpret_cast<intptr_t>(b) - reinterpret_cast<intptr_t>(a);
   if (apart_by >= span(as) || -apart_by >= span(bs)) return false;
-  if (apart_by % size || (tokens > 1 && as[0] != bs[0]) || (heads > 1 && as[1] != bs[1])) return true;
+  if (apart_by % size || (tokens > 1 && as[0] != bs[0]) || (heads > 1 && as[1] != bs[1]))
+    return true;
   struct { int64_t stride, count; } outer{bs[0], tokens}, inner{bs[1], heads};
-  if (outer.count == 1 || (inner.count > 1 && outer.stride < inner.stride)) std::swap(outer, inner);
+  if (outer.count == 1 || (inner.count > 1 && outer.stride < inner.stride))
+    std::swap(outer, inner);
   const auto near = [](auto d, int64_t left, auto use) {   // (of a single row, its own place)
     if (d.count == 1) return use(left);
     const int64_t low = left / d.stride - (left % d.stride < 0);

@@ -246,8 +246,8 @@ __global__ void __launch_bounds__(kThreads) k_append(AppendArgs a, unsigned from
   if ((int)threadIdx.x < held) some[threadIdx.x] = a.offsets[threadIdx.x * stride];
   __syncthreads();
   int at, group;
-  const int64_t t = split(
-      split((int64_t)(from_block + blockIdx.x) * kThreads + threadIdx.x, chunks, &at), groups, &group);
+  const int64_t item = (int64_t)(from_block + blockIdx.x) * kThreads + threadIdx.x;
+  const int64_t t = split(split(item, chunks, &at), groups, &group);
   if (t >= a.k.tokens) return;
   const T* xk = static_cast<const T*>(a.k.x) + t * a.k.xs.outer;
   const T* xv = static_cast<const T*>(a.v) + t * a.vs.outer;
